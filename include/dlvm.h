@@ -460,6 +460,122 @@ dlvm_status dlvm_chain8(int64_t rows, int64_t cols, const float* z,
 dlvm_status dlvm_sgd(int32_t dtype, int64_t n, void* params, float* master,
                      const float* grads, float lr, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Sequence operators: token embeddings, the gated linear recurrence and the
+ * scoring of tokens, the steps that a recurrent language model needs beside
+ * the dense layers. Step-level calls like the ones above. Token ids are int32;
+ * -1 stands for "no token" (padding).
+ * ------------------------------------------------------------------------- */
+
+/* Rows of a table: out[i, :] = scale * table[ids[i], :] (the dense layer of
+ * one-hot rows, without the product). table [vocab, width] and out [tokens,
+ * width] are `dtype`; the product with `scale` is float32, rounded once. A row
+ * whose id is -1 is zero; one whose id is any other value outside [0, vocab)
+ * is NaN. vocab at most 2^24, tokens at most 2^30, scale finite. */
+dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
+                                   const void* table, const int32_t* ids, float scale, void* out,
+                                   void* stream);
+
+/* Gradient of the table: dtable[v, :] = scale * sum of dout[i, :] over the i
+ * with ids[i] == v (float32 [vocab, width]; dout [tokens, width] is `dtype`).
+ * The whole table is written (rows without a token as zero), or, with
+ * `accumulate` 1, the sums are added to it and rows without a token are not
+ * touched (a table shared with the output layer, several batches to a step).
+ * Ids outside [0, vocab) contribute nothing. Tokens are sorted by id first and
+ * a row is summed in the order of its tokens, in parts whose bounds depend on
+ * the ids alone: no floating-point atomics. `ws` needs
+ * dlvm_embedding_backward_ws_bytes (0 for invalid sizes). */
+size_t dlvm_embedding_backward_ws_bytes(int64_t vocab, int64_t width, int64_t tokens);
+dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
+                                    const int32_t* ids, const void* dout, float scale,
+                                    int32_t accumulate, float* dtable, void* ws, size_t ws_bytes,
+                                    void* stream);
+
+/* The gated linear recurrence over `steps` time steps, one state per batch
+ * entry and column: with the gate a = sigmoid(z),
+ *   DLVM_SCAN_FREE:    h_t = a_t * h_{t-1} + x_t
+ *   DLVM_SCAN_COUPLED: h_t = a_t * h_{t-1} + (1 - a_t) * x_t
+ * Time-major like dlvm_rnn_forward: row t * batch + b of z, x and hs holds
+ * step t of batch entry b. Rows have strides ldz, ldx, ldh >= width, so that z
+ * and x may be the two halves of one dense product. z, x, hs are `dtype`;
+ * the state is float32 throughout: h0 [batch, width] (NULL: zeros), hT [batch,
+ * width] (may be NULL) receives the state after the last step. hT may be h0,
+ * updated in place: a call with steps = 1 is one decoding step. Other outputs
+ * must not overlap inputs.
+ * lens (NULL: every sequence has `steps` steps) holds `batch` int32 lengths of
+ * a padded batch, taken as clamped to [0, steps]: steps t >= lens[b] leave the
+ * state as it is, their z and x are not used (whatever they hold) and their hs
+ * rows are zero. Columns width .. ld of a row are not touched.
+ * `ws` (dlvm_gated_scan_ws_bytes, or NULL) lets a call with few columns and
+ * many steps be cut into segments of time that run side by side and are then
+ * joined; with NULL no call is cut. batch * width and batch * steps at most
+ * 2^31 - 1. */
+enum { DLVM_SCAN_FREE = 0, DLVM_SCAN_COUPLED = 1 };
+size_t dlvm_gated_scan_ws_bytes(int32_t dtype, int64_t steps, int64_t batch, int64_t width);
+dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, int64_t batch,
+                                    int64_t width, const void* z, int64_t ldz, const void* x,
+                                    int64_t ldx, const float* h0, const int32_t* lens, void* hs,
+                                    int64_t ldh, float* hT, void* ws, size_t ws_bytes,
+                                    void* stream);
+
+/* Gradient of the recurrence: dhs (row stride lddh, `dtype`; NULL: zeros) holds
+ * the adjoints of hs and dhT (float32; NULL: zeros) that of the last state; one
+ * of them is given. z, x, h0, lens as in the forward call and hs as it wrote
+ * it (the states between are recomputed from a few of its rows). Writes dz and
+ * dx (strides lddz, lddx, `dtype`; they may be the two halves of one buffer)
+ * and, unless NULL, dh0 (float32 [batch, width]; it may be dhT). Rows t >=
+ * lens[b] of dz and dx are zero; those of dhs are not used. */
+dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps, int64_t batch,
+                                     int64_t width, const void* z, int64_t ldz, const void* x,
+                                     int64_t ldx, const float* h0, const int32_t* lens,
+                                     const void* hs, int64_t ldh, const void* dhs, int64_t lddh,
+                                     const float* dhT, void* dz, int64_t lddz, void* dx,
+                                     int64_t lddx, float* dh0, void* ws, size_t ws_bytes,
+                                     void* stream);
+
+/* Scores of tokens under logits [rows, classes] (`dtype`, row stride ld >=
+ * classes): with y = scale * logits (scale > 0 and finite, an inverse
+ * temperature) and p = softmax(y), all outputs float32 unless said:
+ *   logp[i]     y[i, tokens[i]] - lse[i]; 0 where tokens[i] is -1, NaN for any
+ *               other token outside [0, classes). tokens and logp NULL: none.
+ *   lse[i]      logsumexp(y[i, :])                       (may be NULL)
+ *   entropy[i]  -sum_c p_c log p_c, in nats              (may be NULL)
+ *   top_ids [rows, top] int32, top_logp [rows, top]: the `top` classes of the
+ *               largest logits in falling order, the lowest class first among
+ *               equals, and their log probabilities. top in [0, DLVM_TOP_MAX],
+ *               at most classes; 0: both NULL.
+ * Classes masked with -infinity (or the type's lowest value) have probability
+ * 0 and no part in the entropy. A row whose y are all below -1e30 is masked
+ * everywhere: it has lse = logp = top_logp = -infinity and entropy 0. A row with a NaN or +infinity has NaN for
+ * lse, logp, entropy and top_logp; a NaN counts as -infinity in the order of
+ * top_ids. `ws` (dlvm_token_logprobs_ws_bytes, or NULL) lets a call of few
+ * rows cut them into parts that run side by side; with NULL no row is cut. */
+enum { DLVM_TOP_MAX = 32 };
+size_t dlvm_token_logprobs_ws_bytes(int64_t rows, int64_t classes, int32_t top);
+dlvm_status dlvm_token_logprobs(int32_t dtype, int64_t rows, int64_t classes, const void* logits,
+                                int64_t ld, float scale, const int32_t* tokens, float* logp,
+                                float* lse, float* entropy, int32_t top, int32_t* top_ids,
+                                float* top_logp, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of logp and entropy with respect to the logits, for the adjoints
+ * dlogp and dentropy (float32 [rows]; either may be NULL: zeros, not both):
+ *   dlogits[i, c] = scale * (dlogp[i] * ([c == tokens[i]] - p_c)
+ *                            - dentropy[i] * p_c * (log p_c + entropy[i])),
+ * `out_dtype` (F32, or BF16 with either dtype; BF16 logits give BF16), row
+ * stride ld_out, columns classes .. ld_out not touched. lse (and entropy, with
+ * dentropy) as dlvm_token_logprobs wrote them for the same logits and scale.
+ * Rows whose token is -1 (tokens may be NULL without dlogp) take no part of
+ * dlogp; rows whose token is any other value outside [0, classes) are NaN with
+ * dlogp given. A row masked everywhere has a zero gradient. Probabilities are
+ * exp(y - lse), off by half a step of lse. dlogits may be the logits themselves
+ * (same type and stride), overwritten in place. */
+dlvm_status dlvm_token_logprobs_backward(int32_t dtype, int32_t out_dtype, int64_t rows,
+                                         int64_t classes, const void* logits, int64_t ld,
+                                         float scale, const int32_t* tokens, const float* lse,
+                                         const float* entropy, const float* dlogp,
+                                         const float* dentropy, void* dlogits, int64_t ld_out,
+                                         void* stream);
+
 #ifdef __cplusplus
 }
 #endif

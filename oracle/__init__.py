@@ -19,3 +19,5 @@ from .mlp import (MlpSpec, apply_act, chain8, dense_forward, dense_vjp_input,  #
                   sgd_f32, softmax_xent)
 from .rnn import RnnSpec, rnn_forward, rnn_vjp  # noqa: F401
 from .chain import chain_order, chain_product, chain_product_in_order, parenthesisation  # noqa: F401
+from .sequence import (embedding, embedding_grad, gated_scan, gated_scan_vjp, sigmoid,  # noqa: F401
+                       token_scores, token_scores_vjp)

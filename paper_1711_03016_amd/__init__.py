@@ -23,6 +23,8 @@ F32, BF16 = 0, 1
 ACTS = {"none": 0, "sigmoid": 1, "tanh": 2, "relu": 3}
 DTYPES = {"f32": F32, "bf16": BF16}
 LOSSES = {"softmax_ce": 0, "chain8": 1}
+SCAN_MODES = {"free": 0, "coupled": 1}
+TOP_MAX = 32
 WS_HIDDEN, WS_LOGITS, WS_ADJOINT = 0, 1, 2
 
 
@@ -115,6 +117,21 @@ _SIGS = {
     "dlvm_chain_create": (_I32, [_I32, _I32, ctypes.POINTER(_I64), ctypes.POINTER(_I32),
                                  ctypes.POINTER(_P)]),
     "dlvm_chain_run": (_I32, [_P, ctypes.POINTER(_P), _P, _P, ctypes.c_size_t, _P]),
+    "dlvm_embedding_forward": (_I32, [_I32, _I64, _I64, _I64, _P, _P, _F, _P, _P]),
+    "dlvm_embedding_backward_ws_bytes": (ctypes.c_size_t, [_I64, _I64, _I64]),
+    "dlvm_embedding_backward": (_I32, [_I32, _I64, _I64, _I64, _P, _P, _F, _I32, _P, _P,
+                                       ctypes.c_size_t, _P]),
+    "dlvm_gated_scan_ws_bytes": (ctypes.c_size_t, [_I32, _I64, _I64, _I64]),
+    "dlvm_gated_scan_forward": (_I32, [_I32, _I32, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, _P,
+                                       _P, _I64, _P, _P, ctypes.c_size_t, _P]),
+    "dlvm_gated_scan_backward": (_I32, [_I32, _I32, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, _P,
+                                        _P, _I64, _P, _I64, _P, _P, _I64, _P, _I64, _P, _P,
+                                        ctypes.c_size_t, _P]),
+    "dlvm_token_logprobs_ws_bytes": (ctypes.c_size_t, [_I64, _I64, _I32]),
+    "dlvm_token_logprobs": (_I32, [_I32, _I64, _I64, _P, _I64, _F, _P, _P, _P, _P, _I32, _P, _P,
+                                   _P, ctypes.c_size_t, _P]),
+    "dlvm_token_logprobs_backward": (_I32, [_I32, _I32, _I64, _I64, _P, _I64, _F, _P, _P, _P, _P,
+                                            _P, _P, _I64, _P]),
     "dlvm_graph_launch": (_I32, [_P, _P]),
     "dlvm_graph_destroy": (None, [_P]),
 }
@@ -443,6 +460,134 @@ def chain8(rows, cols, z, bias, x_skip, zbar, xbar, loss, ws, stream=None):
 def sgd(dtype, n, params, master, grads, lr, stream=None):
     _check(lib().dlvm_sgd(DTYPES[dtype], int(n), _ptr(params), _ptr(master), _ptr(grads),
                           float(lr), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# sequence operators: token embeddings, gated linear recurrence, token scores
+# ---------------------------------------------------------------------------
+_TYPES = None
+
+
+def _types():
+    """torch types of the storage names, of ids and of workspaces."""
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "i32": torch.int32,
+                  "ws": torch.uint8}
+    return _TYPES
+
+
+def _call(fn, stream, tensors, *args):
+    """`fn(*args, stream)` on the GPU of `tensors`, ((name, tensor or None or address,
+    type name), ...): tensors of another type, on the host or on a second GPU are refused,
+    sizes and strides are the caller's, as in C."""
+    types = _types()
+    dev = None
+    for name, t, ty in tensors:
+        if t is None or isinstance(t, int):
+            continue
+        if t.dtype is not types[ty]:
+            raise DlvmError(ERR_INVALID_ARG, f"{name} is {t.dtype}, not {types[ty]}")
+        d = t.get_device()
+        if d < 0:
+            raise DlvmError(ERR_INVALID_ARG, f"{name} is not in GPU memory")
+        if dev is None:
+            dev = d
+        elif d != dev:
+            raise DlvmError(ERR_INVALID_ARG, f"{name} is on GPU {d}, another tensor on {dev}")
+    import torch
+    if dev is None or dev == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)))
+        return
+    if stream is not None and not isinstance(stream, int) and stream.device.index != dev:
+        raise DlvmError(ERR_INVALID_ARG, f"the stream is not on GPU {dev}")
+    with torch.cuda.device(dev):
+        _check(fn(*args, _stream(stream)))
+
+
+def _ws_args(ws):
+    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+
+
+def embedding_forward(dtype, vocab, width, tokens, table, ids, scale, out, stream=None):
+    """out[i] = scale * table[ids[i]] (``dlvm_embedding_forward``)."""
+    _call(lib().dlvm_embedding_forward, stream,
+          (("table", table, dtype), ("ids", ids, "i32"), ("out", out, dtype)),
+          DTYPES[dtype], vocab, width, tokens, _ptr(table), _ptr(ids), float(scale), _ptr(out))
+
+
+def embedding_backward_ws_bytes(vocab: int, width: int, tokens: int) -> int:
+    return int(lib().dlvm_embedding_backward_ws_bytes(int(vocab), int(width), int(tokens)))
+
+
+def embedding_backward(dtype, vocab, width, tokens, ids, dout, scale, accumulate, dtable, ws,
+                       stream=None):
+    """dtable[v] (+)= scale * the sum of dout[i] over ids[i] == v (``dlvm_embedding_backward``)."""
+    p, n = _ws_args(ws)
+    _call(lib().dlvm_embedding_backward, stream,
+          (("ids", ids, "i32"), ("dout", dout, dtype), ("dtable", dtable, "f32"), ("ws", ws, "ws")),
+          DTYPES[dtype], vocab, width, tokens, _ptr(ids), _ptr(dout), float(scale),
+          int(bool(accumulate)), _ptr(dtable), p, n)
+
+
+def gated_scan_ws_bytes(dtype, steps: int, batch: int, width: int) -> int:
+    return int(lib().dlvm_gated_scan_ws_bytes(DTYPES[dtype], int(steps), int(batch), int(width)))
+
+
+def gated_scan_forward(dtype, mode, steps, batch, width, z, ldz, x, ldx, h0, lens, hs, ldh, hT,
+                       ws=None, stream=None):
+    """h_t = a_t h_{t-1} + x_t ("free") or + (1 - a_t) x_t ("coupled"), a = sigmoid(z)
+    (``dlvm_gated_scan_forward``); h0, lens, hT and ws may be None."""
+    p, n = _ws_args(ws)
+    _call(lib().dlvm_gated_scan_forward, stream,
+          (("z", z, dtype), ("x", x, dtype), ("h0", h0, "f32"), ("lens", lens, "i32"),
+           ("hs", hs, dtype), ("hT", hT, "f32"), ("ws", ws, "ws")),
+          DTYPES[dtype], SCAN_MODES[mode], steps, batch, width, _ptr(z), ldz, _ptr(x), ldx,
+          _ptr(h0), _ptr(lens), _ptr(hs), ldh, _ptr(hT), p, n)
+
+
+def gated_scan_backward(dtype, mode, steps, batch, width, z, ldz, x, ldx, h0, lens, hs, ldh, dhs,
+                        lddh, dhT, dz, lddz, dx, lddx, dh0, ws=None, stream=None):
+    """Gradient of the recurrence for the adjoints dhs of hs and dhT of the last state
+    (``dlvm_gated_scan_backward``); h0, lens, one of dhs and dhT, dh0 and ws may be None."""
+    p, n = _ws_args(ws)
+    _call(lib().dlvm_gated_scan_backward, stream,
+          (("z", z, dtype), ("x", x, dtype), ("h0", h0, "f32"), ("lens", lens, "i32"),
+           ("hs", hs, dtype), ("dhs", dhs, dtype), ("dhT", dhT, "f32"), ("dz", dz, dtype),
+           ("dx", dx, dtype), ("dh0", dh0, "f32"), ("ws", ws, "ws")),
+          DTYPES[dtype], SCAN_MODES[mode], steps, batch, width, _ptr(z), ldz, _ptr(x), ldx,
+          _ptr(h0), _ptr(lens), _ptr(hs), ldh, _ptr(dhs), lddh, _ptr(dhT), _ptr(dz), lddz,
+          _ptr(dx), lddx, _ptr(dh0), p, n)
+
+
+def token_logprobs_ws_bytes(rows: int, classes: int, top: int) -> int:
+    return int(lib().dlvm_token_logprobs_ws_bytes(int(rows), int(classes), int(top)))
+
+
+def token_logprobs(dtype, rows, classes, logits, ld, scale, tokens, logp, lse, entropy, top,
+                   top_ids, top_logp, ws=None, stream=None):
+    """Log probabilities of tokens, log-sum-exp, entropy and the `top` largest alternatives
+    of each row (``dlvm_token_logprobs``); outputs not wanted are None."""
+    p, n = _ws_args(ws)
+    _call(lib().dlvm_token_logprobs, stream,
+          (("logits", logits, dtype), ("tokens", tokens, "i32"), ("logp", logp, "f32"),
+           ("lse", lse, "f32"), ("entropy", entropy, "f32"), ("top_ids", top_ids, "i32"),
+           ("top_logp", top_logp, "f32"), ("ws", ws, "ws")),
+          DTYPES[dtype], rows, classes, _ptr(logits), ld, float(scale), _ptr(tokens), _ptr(logp),
+          _ptr(lse), _ptr(entropy), top, _ptr(top_ids), _ptr(top_logp), p, n)
+
+
+def token_logprobs_backward(dtype, out_dtype, rows, classes, logits, ld, scale, tokens, lse,
+                            entropy, dlogp, dentropy, dlogits, ld_out, stream=None):
+    """Gradient of logp and entropy with respect to the logits
+    (``dlvm_token_logprobs_backward``); dlogp or dentropy may be None."""
+    _call(lib().dlvm_token_logprobs_backward, stream,
+          (("logits", logits, dtype), ("tokens", tokens, "i32"), ("lse", lse, "f32"),
+           ("entropy", entropy, "f32"), ("dlogp", dlogp, "f32"), ("dentropy", dentropy, "f32"),
+           ("dlogits", dlogits, out_dtype)),
+          DTYPES[dtype], DTYPES[out_dtype], rows, classes, _ptr(logits), ld, float(scale),
+          _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), ld_out)
 
 
 # ---------------------------------------------------------------------------

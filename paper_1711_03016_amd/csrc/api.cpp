@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "dlvm.h"
+#include "api_common.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -28,6 +29,7 @@ using dlvm::GemmDesc;
 using dlvm::Layout;
 using dlvm::PacketEvents;
 using dlvm::packet_events;
+using namespace dlvm::api;
 
 dlvm::PacketEvents& dlvm::packet_events() {
   thread_local PacketEvents e;
@@ -80,24 +82,6 @@ struct dlvm_graph {
 
 namespace {
 
-thread_local std::string g_last_error;
-
-dlvm_status fail(dlvm_status code, const std::string& msg) {
-  g_last_error = msg;
-  return code;
-}
-
-dlvm_status hip_fail(hipError_t e, const char* where) {
-  return fail(DLVM_ERR_HIP, std::string(where) + ": " + hipGetErrorString(e));
-}
-
-constexpr size_t kAlign = 256;
-size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-size_t elem_size(int dtype) { return dtype == DLVM_BF16 ? 2 : 4; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool valid_dtype(int32_t d) { return d == DLVM_F32 || d == DLVM_BF16; }
-bool valid_act(int32_t a) { return a >= DLVM_ACT_NONE && a <= DLVM_ACT_RELU; }
-
 // Workspace layout for a given batch. Offsets in bytes from the base.
 struct WsLayout {
   size_t flags = 0;         // int32[4]: [0] label out of range, [1] non-finite loss
@@ -121,11 +105,6 @@ GemmDesc gemm_tn(int dtype, int64_t M, int64_t N, int64_t K, const void* X, cons
 GemmDesc gemm_nn(int dtype, int out_dtype, int act, int64_t M, int64_t N, int64_t K, float alpha,
                  const void* X, const void* W, int64_t ldw, const void* bias, void* H,
                  int64_t ldh);
-
-// Address arithmetic on integers: a dry run (plan description) uses null bases.
-template <typename T> T* at(const void* base, size_t off) {
-  return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(base) + off);
-}
 
 const void* param_ptr(const dlvm_model* m, const void* params, int64_t elem_off) {
   return at<const void>(params, static_cast<size_t>(elem_off) * elem_size(m->dtype));

@@ -1,0 +1,235 @@
+"""The sequence operators together, as a recurrent language model uses them: tokens are
+looked up, one dense product makes gates and inputs, the recurrence runs over time, a
+dense product makes logits, the given tokens are scored, and the adjoints go all the way
+back. Against an independent library's float64 autograd of the same model; captured into
+a graph; on two streams at once; and token by token.
+
+Tolerances: float32 as everywhere in the tests (1e-4). In bf16 every stage of the way
+rounds what it stores by at most 2^-8 of it: six stages forward and four back.
+"""
+import numpy as np
+import pytest
+
+import paper_1711_03016_amd as dl
+from helpers import TOL, assert_close, device, quant, to_dev, to_np, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+STAGES = 10
+TOLS = {"f32": TOL["f32"], "bf16": STAGES * 2.0 ** -8}
+
+
+class Net:
+    """V tokens, E wide embeddings, H states, on B sequences of T tokens."""
+
+    def __init__(self, dtype, V, E, H, T, B, seed, lens=None):
+        import torch
+        r = np.random.default_rng([808, seed])
+        self.dtype, self.V, self.E, self.H, self.T, self.B = dtype, V, E, H, T, B
+        n = T * B
+        self.host = dict(
+            table=r.standard_normal((V, E)), w=r.standard_normal((E, 2 * H)) / np.sqrt(E),
+            b=np.concatenate([np.full(H, 1.0), np.zeros(H)]),
+            wo=r.standard_normal((H, V)) / np.sqrt(H), bo=r.standard_normal(V) * 0.1,
+            h0=r.standard_normal((B, H)) * 0.5)
+        self.host = {k: v.astype(np.float32) for k, v in self.host.items()}
+        self.ids = r.integers(0, V, n).astype(np.int32)
+        self.next = r.integers(0, V, n).astype(np.int32)
+        self.lens = lens
+        if lens is not None:
+            dead = (np.arange(T)[:, None] >= np.asarray(lens)).reshape(-1)
+            self.ids[dead] = -1
+            self.next[dead] = -1
+        self.gl = (-np.ones(n) / n).astype(np.float32)
+        self.ge = np.full(n, -0.05 / n, np.float32)
+        self.d = {k: to_dev(v, "f32" if k == "h0" else dtype) for k, v in self.host.items()}
+        dev = lambda a: torch.from_numpy(a).to(device())  # noqa: E731
+        self.di, self.dn, self.dgl, self.dge = dev(self.ids), dev(self.next), dev(self.gl), dev(self.ge)
+        self.dl = None if lens is None else dev(np.asarray(lens, np.int32))
+        td = torch_dtype(dtype)
+        e = lambda *s, t=td: torch.full(s, float("nan"), dtype=t, device=device())  # noqa: E731
+        f = torch.float32
+        self.o = dict(x=e(n, E), zx=e(n, 2 * H), hs=e(n, H), hT=e(B, H, t=f), logits=e(n, V, t=f),
+                      logp=e(n, t=f), lse=e(n, t=f), entropy=e(n, t=f), dlogits=e(n, V), dhs=e(n, H),
+                      dwo=e(H, V, t=f), dbo=e(V, t=f), dzx=e(n, 2 * H), dh0=e(B, H, t=f), dx=e(n, E),
+                      dw=e(E, 2 * H, t=f), db=e(2 * H, t=f), dtable=e(V, E, t=f))
+        u = lambda b: torch.full((b,), 255, dtype=torch.uint8, device=device())  # noqa: E731
+        self.ws = [u(dl.gated_scan_ws_bytes(dtype, T, B, H)), u(dl.token_logprobs_ws_bytes(n, V, 0)),
+                   u(dl.embedding_backward_ws_bytes(V, E, n))]
+
+    def step(self, stream=None):
+        dt, n, E, H, V, T, B, d, o = self.dtype, self.T * self.B, self.E, self.H, self.V, self.T, self.B, self.d, self.o
+        s = stream
+        dl.embedding_forward(dt, V, E, n, d["table"], self.di, 1.0, o["x"], s)
+        dl.dense_forward(dt, dt, "none", n, 2 * H, E, 1.0, o["x"], d["w"], d["b"], o["zx"], s)
+        z, x = o["zx"][:, :H], o["zx"][:, H:]
+        dl.gated_scan_forward(dt, "coupled", T, B, H, z, 2 * H, x, 2 * H, d["h0"], self.dl, o["hs"], H,
+                              o["hT"], self.ws[0], s)
+        dl.dense_forward(dt, "f32", "none", n, V, H, 1.0, o["hs"], d["wo"], d["bo"], o["logits"], s)
+        dl.token_logprobs("f32", n, V, o["logits"], V, 1.0, self.dn, o["logp"], o["lse"], o["entropy"], 0,
+                          None, None, self.ws[1], s)
+        dl.token_logprobs_backward("f32", dt, n, V, o["logits"], V, 1.0, self.dn, o["lse"], o["entropy"],
+                                   self.dgl, self.dge, o["dlogits"], V, s)
+        dl.dense_backward_params(dt, n, V, H, o["hs"], o["dlogits"], o["dwo"], o["dbo"], s)
+        dl.dense_backward_data(dt, dt, "none", n, V, H, o["dlogits"], d["wo"], None, None, o["dhs"], s)
+        dl.gated_scan_backward(dt, "coupled", T, B, H, z, 2 * H, x, 2 * H, d["h0"], self.dl, o["hs"], H,
+                               o["dhs"], H, None, o["dzx"][:, :H], 2 * H, o["dzx"][:, H:], 2 * H, o["dh0"],
+                               self.ws[0], s)
+        dl.dense_backward_params(dt, n, 2 * H, E, o["x"], o["dzx"], o["dw"], o["db"], s)
+        dl.dense_backward_data(dt, dt, "none", n, 2 * H, E, o["dzx"], d["w"], None, None, o["dx"], s)
+        dl.embedding_backward(dt, V, E, n, self.di, o["dx"], 1.0, False, o["dtable"], self.ws[2], s)
+
+    def reference(self):
+        import torch
+        p = {k: torch.tensor(quant(v, "f32" if k == "h0" else self.dtype), requires_grad=True)
+             for k, v in self.host.items()}
+        ids = torch.from_numpy(self.ids.astype(np.int64))
+        x = torch.where((ids >= 0)[:, None], p["table"][ids.clamp(min=0)], 0.0)
+        zx = (x @ p["w"] + p["b"]).view(self.T, self.B, 2 * self.H)
+        h, hs = p["h0"], []
+        n = np.full(self.B, self.T) if self.lens is None else np.asarray(self.lens)
+        for t in range(self.T):
+            a = torch.sigmoid(zx[t, :, :self.H])
+            new = a * h + (1 - a) * zx[t, :, self.H:]
+            on = torch.from_numpy(t < n)[:, None]
+            h = torch.where(on, new, h)
+            hs.append(torch.where(on, new, 0.0))
+        out = {"hT": h}
+        hs = torch.stack(hs).view(-1, self.H)
+        lp = torch.log_softmax(hs @ p["wo"] + p["bo"], 1)
+        nx = torch.from_numpy(self.next.astype(np.int64))
+        logp = torch.where(nx >= 0, lp.gather(1, nx.clamp(min=0)[:, None])[:, 0], 0.0)
+        ent = -(lp.exp() * lp).sum(1)
+        ((logp * torch.from_numpy(self.gl)).sum() + (ent * torch.from_numpy(self.ge)).sum()).backward()
+        out |= {"hs": hs, "logp": logp, "entropy": ent}
+        out = {k: v.detach().numpy() for k, v in out.items()}
+        for name, k in (("table", "dtable"), ("w", "dw"), ("b", "db"), ("wo", "dwo"), ("bo", "dbo"), ("h0", "dh0")):
+            out[k] = p[name].grad.numpy()
+        return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(97, 48, 64, 24, 3, None), (1000, 64, 40, 130, 2, None),
+                                  (300, 72, 56, 17, 5, (17, 0, 1, 9, 16)), (50, 8, 8, 1, 4, None)])
+def test_training_step(dtype, size):
+    net = Net(dtype, *size[:5], seed=1, lens=size[5])
+    net.step()
+    ref = net.reference()
+    for k, v in ref.items():
+        assert_close(to_np(net.o[k]), v, TOLS[dtype], k, row_tol=4 * TOLS[dtype], floor=1.0)
+
+
+def test_captured_and_replayed():
+    """One graph of the whole step: every replay gives the eager step's bits, with the
+    program's own work between, new tokens and weights in place included."""
+    import torch
+    net, other = Net("bf16", 300, 64, 56, 70, 3, seed=2), Net("bf16", 300, 64, 56, 70, 3, seed=3)
+    net.step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        net.step()
+    inputs = [(net.di, net.dn, net.d["table"], net.d["wo"]), (other.di, other.dn, other.d["table"], other.d["wo"])]
+    first = [t.clone() for t in inputs[0]]
+    for i in range(4):
+        for t, new in zip(inputs[0], inputs[1] if i % 2 else first):
+            t.copy_(new)
+        net.step()
+        torch.cuda.synchronize()
+        want = {k: v.clone() for k, v in net.o.items()}
+        for v in net.o.values():
+            v.fill_(float("nan"))
+        other.step()
+        for w in net.ws:
+            w.fill_(i)
+        g.replay()
+        torch.cuda.synchronize()
+        for k, v in net.o.items():
+            assert torch.equal(v, want[k]), (i, k)
+
+
+def test_two_streams_at_once():
+    import torch
+    nets = [Net("bf16", 500, 64, 128, 200, 2, seed=4), Net("f32", 400, 40, 72, 150, 3, seed=5)]
+    for n in nets:
+        n.step()
+    torch.cuda.synchronize()
+    want = [{k: v.clone() for k, v in n.o.items()} for n in nets]
+    for n in nets:
+        for v in n.o.values():
+            v.fill_(float("nan"))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for n, s in zip(nets, streams):
+            n.step(s)
+    torch.cuda.synchronize()
+    for n, w in zip(nets, want):
+        for k, v in n.o.items():
+            assert torch.equal(v, w[k]), k
+
+
+def test_tokens_into_the_recurrent_cell():
+    """Embeddings as the recurrent cell's inputs, and their gradient from its dxs."""
+    import oracle
+    import torch
+    V, Kx, H, T, B = 60, 32, 40, 6, 8
+    r = np.random.default_rng([809])
+    table = r.standard_normal((V, Kx)).astype(np.float32)
+    W, U = (r.standard_normal((k, H)).astype(np.float32) / np.sqrt(k) for k in (Kx, H))
+    b = r.standard_normal(H).astype(np.float32) * 0.1
+    ids = r.integers(0, V, T * B).astype(np.int32)
+    dhs = r.standard_normal((T, B, H)).astype(np.float32)
+    m = dl.Rnn(T, Kx, H, "tanh", "f32", wrt_x=True, wrt_h0=False, batch_max=B)
+    P = m.pack_cell(W, U, b, device(), torch.float32)
+    xs = torch.empty((T, B, Kx), device=device())
+    di = torch.from_numpy(ids).to(device())
+    dl.embedding_forward("f32", V, Kx, T * B, to_dev(table), di, 1.0, xs)
+    hs = torch.zeros((T + 1, B, H), device=device())
+    ws = torch.empty(m.workspace_bytes(B), dtype=torch.uint8, device=device())
+    m.forward(P, xs, B, hs, ws)
+    dP, dxs = torch.empty(m.param_count(), device=device()), torch.empty((T, B, Kx), device=device())
+    m.backward(P, xs, hs, to_dev(dhs), B, dP, dxs, None, ws)
+    dtable = torch.empty((V, Kx), device=device())
+    we = torch.empty(dl.embedding_backward_ws_bytes(V, Kx, T * B), dtype=torch.uint8, device=device())
+    dl.embedding_backward("f32", V, Kx, T * B, di, dxs.view(T * B, Kx), 1.0, False, dtable, we)
+    t = {k: torch.tensor(v.astype(np.float64), requires_grad=True) for k, v in dict(e=table, W=W, U=U).items()}
+    h, loss = torch.zeros((B, H), dtype=torch.float64), 0.0
+    x = t["e"][torch.from_numpy(ids.astype(np.int64))].view(T, B, Kx)
+    for i in range(T):
+        h = torch.tanh(x[i] @ t["W"] + h @ t["U"] + torch.from_numpy(b).double())
+        loss = loss + (h * torch.from_numpy(dhs[i]).double()).sum()
+    loss.backward()
+    assert_close(to_np(hs[T]), h.detach().numpy(), TOL["f32"])
+    assert_close(to_np(dtable), t["e"].grad.numpy(), TOL["f32"], row_tol=4 * TOL["f32"])
+    ref, _, _ = oracle.embedding_grad(to_np(dxs.view(T * B, Kx)), ids, V, 1.0)
+    assert_close(to_np(dtable), ref, 1e-6)
+
+
+def test_token_by_token():
+    """Serving: each token through the lookup, one step of the state in place, and the
+    choice of the next among the alternatives, as the whole sequence at once."""
+    import torch
+    net = Net("f32", 200, 40, 64, 12, 3, seed=6)
+    net.step()
+    B, H, V = net.B, net.H, net.V
+    state = net.d["h0"].clone()
+    x, zx, hs = torch.empty((B, net.E), device=device()), torch.empty((B, 2 * H), device=device()), torch.empty((B, H), device=device())
+    logits = torch.empty((B, V), device=device())
+    logp, ids = torch.empty(B, device=device()), torch.empty((B, 5), dtype=torch.int32, device=device())
+    tlp = torch.empty((B, 5), device=device())
+    ws = torch.empty(dl.token_logprobs_ws_bytes(B, V, 5), dtype=torch.uint8, device=device())
+    for t in range(net.T):
+        # rows of a batch of ids start on 16 bytes only every fourth one: a copy
+        now, nxt = net.di[t * B:(t + 1) * B].clone(), net.dn[t * B:(t + 1) * B].clone()
+        dl.embedding_forward("f32", V, net.E, B, net.d["table"], now, 1.0, x)
+        dl.dense_forward("f32", "f32", "none", B, 2 * H, net.E, 1.0, x, net.d["w"], net.d["b"], zx)
+        dl.gated_scan_forward("f32", "coupled", 1, B, H, zx, 2 * H, zx[:, H:], 2 * H, state, None, hs, H, state)
+        dl.dense_forward("f32", "f32", "none", B, V, H, 1.0, hs, net.d["wo"], net.d["bo"], logits)
+        dl.token_logprobs("f32", B, V, logits, V, 1.0, nxt, logp, None, None, 5, ids, tlp, ws)
+        assert_close(to_np(logp), to_np(net.o["logp"][t * B:(t + 1) * B]), TOL["f32"])
+        full = torch.log_softmax(logits.double(), 1)
+        v, i = full.topk(5, dim=1)
+        assert torch.equal(i.int(), ids)
+        assert_close(to_np(tlp), v.cpu().numpy(), 1e-5)
+    assert_close(to_np(state), to_np(net.o["hT"]), TOL["f32"])
