@@ -471,7 +471,8 @@ dlvm_status dlvm_sgd(int32_t dtype, int64_t n, void* params, float* master,
  * one-hot rows, without the product). table [vocab, width] and out [tokens,
  * width] are `dtype`; the product with `scale` is float32, rounded once. A row
  * whose id is -1 is zero; one whose id is any other value outside [0, vocab)
- * is NaN. vocab at most 2^24, tokens at most 2^30, scale finite. */
+ * is NaN. vocab at most 2^24, width at most 2^20, tokens at most 2^30, scale
+ * finite. */
 dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
                                    const void* table, const int32_t* ids, float scale, void* out,
                                    void* stream);

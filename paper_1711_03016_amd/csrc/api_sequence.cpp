@@ -15,7 +15,7 @@ namespace {
 
 constexpr int64_t kMaxVocab = int64_t(1) << 24;
 constexpr int64_t kMaxTokens = int64_t(1) << 30;
-constexpr int64_t kMaxWidth = int64_t(1) << 24;
+constexpr int64_t kMaxWidth = int64_t(1) << 20;
 constexpr int64_t kMaxRows = INT32_MAX;
 // Strides beyond this could take a row's offset past 63 bits.
 constexpr int64_t kMaxStride = int64_t(1) << 31;
@@ -25,7 +25,7 @@ dlvm_status embedding_sizes(int32_t dtype, int64_t vocab, int64_t width, int64_t
   if (vocab < 1 || width < 1 || tokens < 1) return fail(DLVM_ERR_INVALID_ARG, "sizes must be positive");
   if (!std::isfinite(scale)) return fail(DLVM_ERR_INVALID_ARG, "scale must be finite");
   if (vocab > kMaxVocab || width > kMaxWidth || tokens > kMaxTokens)
-    return fail(DLVM_ERR_UNSUPPORTED, "vocab and width at most 2^24, tokens at most 2^30");
+    return fail(DLVM_ERR_UNSUPPORTED, "vocab at most 2^24, width at most 2^20, tokens at most 2^30");
   return DLVM_OK;
 }
 

@@ -38,7 +38,7 @@ LOOKUP = dict(dtype=0, vocab=10, width=4, tokens=3, table=A, ids=A, scale=1.0, o
     (dict(tokens=0), INV), (dict(tokens=-1), INV), (dict(scale=math.nan), INV),
     (dict(scale=math.inf), INV), (dict(table=None), INV), (dict(ids=None), INV), (dict(out=None), INV),
     (dict(table=ODD), MIS), (dict(ids=ODD), MIS), (dict(out=ODD), MIS),
-    (dict(vocab=(1 << 24) + 1), UNS), (dict(width=(1 << 24) + 1), UNS), (dict(tokens=(1 << 30) + 1), UNS),
+    (dict(vocab=(1 << 24) + 1), UNS), (dict(width=(1 << 20) + 1), UNS), (dict(tokens=(1 << 30) + 1), UNS),
 ])
 def test_embedding_forward_refuses(changes, status):
     assert _call("dlvm_embedding_forward", LOOKUP, changes) == status
