@@ -483,8 +483,8 @@ dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, 
  * `accumulate` 1, the sums are added to it and rows without a token are not
  * touched (a table shared with the output layer, several batches to a step).
  * Ids outside [0, vocab) contribute nothing. Tokens are sorted by id first and
- * a row is summed in the order of its tokens, in parts whose bounds depend on
- * the ids alone: no floating-point atomics. `ws` needs
+ * a row is summed in an order and in parts that depend on the ids alone: no
+ * floating-point atomics. `ws` needs
  * dlvm_embedding_backward_ws_bytes (0 for invalid sizes). */
 size_t dlvm_embedding_backward_ws_bytes(int64_t vocab, int64_t width, int64_t tokens);
 dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
