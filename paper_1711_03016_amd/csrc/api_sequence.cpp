@@ -29,13 +29,17 @@ dlvm_status embedding_sizes(int32_t dtype, int64_t vocab, int64_t width, int64_t
   return DLVM_OK;
 }
 
+bool scan_fits(int64_t steps, int64_t batch, int64_t width) {
+  return steps <= (int64_t(1) << 30) && batch <= INT32_MAX && width <= INT32_MAX &&
+         batch * width <= INT32_MAX && batch * steps <= INT32_MAX;
+}
+
 dlvm_status scan_sizes(int32_t dtype, int32_t mode, int64_t steps, int64_t batch, int64_t width) {
   if (!valid_dtype(dtype)) return fail(DLVM_ERR_INVALID_ARG, "bad dtype");
   if (mode != DLVM_SCAN_FREE && mode != DLVM_SCAN_COUPLED) return fail(DLVM_ERR_INVALID_ARG, "bad mode");
   if (steps < 1 || batch < 1 || width < 1) return fail(DLVM_ERR_INVALID_ARG, "sizes must be positive");
-  if (steps > INT32_MAX || batch > INT32_MAX || width > INT32_MAX || batch * width > INT32_MAX ||
-      batch * steps > INT32_MAX)
-    return fail(DLVM_ERR_UNSUPPORTED, "batch * width and batch * steps at most 2^31 - 1");
+  if (!scan_fits(steps, batch, width))
+    return fail(DLVM_ERR_UNSUPPORTED, "batch * width and batch * steps at most 2^31 - 1, steps at most 2^30");
   return DLVM_OK;
 }
 
@@ -104,8 +108,7 @@ dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width,
 }
 
 size_t dlvm_gated_scan_ws_bytes(int32_t dtype, int64_t steps, int64_t batch, int64_t width) {
-  if (!valid_dtype(dtype) || steps < 1 || batch < 1 || width < 1 || steps > INT32_MAX ||
-      batch > INT32_MAX || width > INT32_MAX || batch * width > INT32_MAX || batch * steps > INT32_MAX)
+  if (!valid_dtype(dtype) || steps < 1 || batch < 1 || width < 1 || !scan_fits(steps, batch, width))
     return 0;
   return dlvm::gated_scan_ws(dtype, steps, batch, width);
 }
