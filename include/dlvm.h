@@ -510,7 +510,7 @@ dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width,
  * `ws` (dlvm_gated_scan_ws_bytes, or NULL) lets a call with few columns and
  * many steps be cut into segments of time that run side by side and are then
  * joined; with NULL no call is cut. batch * width and batch * steps at most
- * 2^31 - 1, steps at most 2^30. */
+ * 2^31 - 1, steps at most 2^30, strides times (63 / width + 1) below 2^30. */
 enum { DLVM_SCAN_FREE = 0, DLVM_SCAN_COUPLED = 1 };
 size_t dlvm_gated_scan_ws_bytes(int32_t dtype, int64_t steps, int64_t batch, int64_t width);
 dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, int64_t batch,

@@ -45,7 +45,9 @@ dlvm_status scan_sizes(int32_t dtype, int32_t mode, int64_t steps, int64_t batch
 
 dlvm_status scan_stride(int64_t ld, int64_t width) {
   if (ld < width) return fail(DLVM_ERR_INVALID_ARG, "row strides must be at least the width");
-  if (ld > kMaxStride) return fail(DLVM_ERR_UNSUPPORTED, "row strides at most 2^31");
+  // the rows that 64 neighbouring states lie in are addressed with 32 bits
+  if (ld > kMaxStride || (63 / width + 1) * ld > (int64_t(1) << 30) - 1)
+    return fail(DLVM_ERR_UNSUPPORTED, "row strides times the rows that hold 64 states at most 2^30");
   return DLVM_OK;
 }
 

@@ -8,7 +8,6 @@
 // sums of rows that run over a piece's end are joined in the order of the pieces.
 #include <math.h>
 
-
 #include "common.hpp"
 #include "kernels.hpp"
 #include "sequence.hpp"

@@ -3,16 +3,17 @@
 //
 // A step is the map h -> a h + u; maps compose, (A2, U2) after (A1, U1) being
 // (A2 A1, A2 U1 + U2), so a stretch of time is summed up by one pair of numbers for each
-// state. The adjoint is the same recurrence backwards: mu -> a (mu + dh). Both calls
-// read their tensors once where there are states enough to fill the GPU:
-//  - many states, or few steps: a thread takes its states through all steps;
-//  - else a workgroup takes 64 V states, its eight waves eight steps each of every 64:
-//    each sums its steps up in registers, the sums are exchanged through LDS, and each
-//    goes through its steps again from the state before them;
-//  - few states and many steps: time is cut into segments besides. A first launch sums
-//    every segment up, and the second starts each from the sums before it. That reads the
-//    inputs a second time, from the Infinity Cache as far as they fit: the second launch
-//    begins with the segments that the first read last.
+// state. The adjoint is the same recurrence backwards: mu -> a (mu + dh). Every variant
+// reads its tensors once, one state to a lane (wider vectors leave fewer waves: 63
+// against 45 us with four states of bf16 to a lane, T = 32, 2^20 states):
+//  - ALONE, many states or few steps: a thread takes its state through all steps;
+//  - SHARED: a workgroup takes 64 states, its eight waves equal numbers of steps of each
+//    block of time: each wave sums its steps up in registers, the sums are exchanged
+//    through LDS, and each goes through its steps again from the state before them;
+//  - SHARED in segments of time, few states and many steps: a first launch sums every
+//    segment up, and the second starts each from the sums before it. That reads half of
+//    the inputs a second time, from the Infinity Cache as far as they fit: the second
+//    launch begins with the segments that the first read last.
 // What bounds them is memory; the arithmetic (two transcendental functions to an element)
 // takes about half of what the vector units could do in that time.
 #include <math.h>
@@ -24,13 +25,10 @@
 namespace dlvm {
 namespace {
 
-constexpr int kUnroll = 8;  // steps of a thread that are in flight together
+enum Mode { ALONE, SHARED };
 constexpr int kWaves = 8;   // waves of a workgroup that share the steps
 
-// V neighbouring states of a row (rows start on V elements).
-template <typename E, int V> struct alignas(sizeof(E) * V) Cols {
-  E v[V];
-};
+constexpr int kUnroll = 8;  // steps of a thread that are in flight together
 
 // a = sigmoid(z) and c = 1 - a, each to float32 accuracy on its own (1 - a from a
 // rounded a loses its digits where the gate is open). z of +-infinity gives 0 and 1, NaN
@@ -47,7 +45,7 @@ __device__ __forceinline__ int32_t length_of(const int32_t* lens, int32_t b, int
   return n < 0 ? 0 : n > T ? static_cast<int32_t>(T) : n;
 }
 
-// Segments of time of one call. sums[s * N + j] is what segment s does to state j.
+// Segments of time of one call. sums[s * N + j] is the map of segment s for state j.
 struct Cut {
   int S;               // segments (1: none)
   int32_t len;         // steps of one
@@ -56,268 +54,300 @@ struct Cut {
   float2* sums;
 };
 
-// Of a thread: its first state, batch entry and column.
+// Of a thread: whether it has a state, which, and the state's batch entry and column;
+// b0 and c0 are those of the wave's first lane. (A lane without a state has the first's.)
 struct Place {
   bool on;
-  int32_t j, b, c;
+  int32_t j, b, c, b0, c0;
 };
-template <int V> __device__ __forceinline__ Place place_of(int tile, int lane, const GatedScan& k) {
+__device__ __forceinline__ Place place_of(int tile, int lane, const GatedScan& k) {
   Place p;
-  const int64_t j = (static_cast<int64_t>(tile) * 64 + lane) * V;
-  p.on = j < k.B * k.H;
-  p.j = p.on ? static_cast<int32_t>(j) : 0;
-  p.b = p.j / static_cast<int32_t>(k.H);
-  p.c = p.j - p.b * static_cast<int32_t>(k.H);
+  const int32_t H = static_cast<int32_t>(k.H);
+  const int32_t first = tile * 64;
+  p.on = static_cast<int64_t>(first) + lane < k.B * k.H;
+  p.j = p.on ? first + lane : first;
+  p.b0 = first / H;
+  p.c0 = first - p.b0 * H;
+  p.b = p.j / H;
+  p.c = p.j - p.b * H;
   return p;
 }
 
-template <typename E, int V>
-__device__ __forceinline__ Cols<E, V> load_cols(const E* p) {
-  return *reinterpret_cast<const Cols<E, V>*>(p);
+// The rows of one tensor as a wave sees them: a scalar address for each step, and the
+// lane's distance from the first lane's element, which fits 32 bits (checked by the
+// caller), so that the addresses of many loads in flight take no vector registers.
+template <typename E> struct Rows {
+  typedef __attribute__((address_space(1))) char Byte;
+  typedef __attribute__((address_space(1))) E Elem;
+  Byte* base;
+  int64_t step;
+  uint32_t at;
+  __device__ __forceinline__ Rows(const void* t, int64_t ld, int64_t B, const Place& p)
+      : base((Byte*)(static_cast<E*>(const_cast<void*>(t)) + (p.b0 * ld + p.c0))),
+        step(B * ld * static_cast<int64_t>(sizeof(E))),
+        at(static_cast<uint32_t>((p.b - p.b0) * ld + p.c - p.c0) * static_cast<uint32_t>(sizeof(E))) {}
+  __device__ __forceinline__ Byte* row(int32_t t) const { return base + t * step; }
+  __device__ __forceinline__ Elem& in(Byte* row) const {
+    asm("" : "+s"(row));  // keeps the scalar part of the address apart from the lane's
+    return *(Elem*)(row + at);
+  }
+};
+
+// The largest of the wave's values.
+__device__ __forceinline__ int32_t wave_max(int32_t v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const int32_t w = __shfl_xor(v, o, 64);
+    v = w > v ? w : v;
+  }
+  return __builtin_amdgcn_readfirstlane(v);
 }
 
 // ---------------------------------------------------------------------------
-// Forward. NW is kWaves, or 1 for a thread that takes its states alone.
+// Forward.
 // ---------------------------------------------------------------------------
-template <typename E, bool COUPLED, int V, int NW>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_gated_scan_kernel(GatedScan k, Cut cut) {
-  constexpr int U = kUnroll;
-  __shared__ float2 sums[2][NW == 1 ? 1 : NW][NW == 1 ? 1 : 64 * V];
+template <typename E, bool COUPLED, int MODE>
+__global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_scan_kernel(GatedScan k, Cut cut) {
+  constexpr int U = kUnroll, NW = MODE == ALONE ? 1 : kWaves;
+  __shared__ float2 sums[2][NW][MODE == ALONE ? 1 : 64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  const int w = NW == 1 ? 0 : wave;
-  const int s = cut.S - 1 - static_cast<int>(blockIdx.x) / cut.tiles;
+  const int w = MODE == ALONE ? 0 : wave;
   const int block = static_cast<int>(blockIdx.x) % cut.tiles;
-  const Place p = place_of<V>(NW == 1 ? block * 4 + wave : block, lane, k);
-  if (NW == 1 && !p.on) return;
+  const int s = cut.S - 1 - static_cast<int>(blockIdx.x) / cut.tiles;
+  const Place p = place_of(MODE == ALONE ? block * 4 + wave : block, lane, k);
+  if (MODE == ALONE && !p.on) return;
+  const int64_t N = k.B * k.H;
+  const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;
-  const int32_t end = k.T - begin < cut.len ? static_cast<int32_t>(k.T) : begin + cut.len;
+  const int32_t end = T - begin < cut.len ? T : begin + cut.len;
   const int32_t n = length_of(k.lens, p.b, k.T);
   const int32_t live = !p.on ? 0 : n < end ? n : end;  // steps below it are read
-  const E* pz = static_cast<const E*>(k.z) + p.b * k.ldz + p.c;
-  const E* px = static_cast<const E*>(k.x) + p.b * k.ldx + p.c;
-  E* ph = static_cast<E*>(k.hs) + p.b * k.ldh + p.c;
-  const int64_t sz = k.B * k.ldz, sx = k.B * k.ldx, sh = k.B * k.ldh;
+  const Rows<E> pz(k.z, k.ldz, k.B, p), px(k.x, k.ldx, k.B, p), ph(k.hs, k.ldh, k.B, p);
 
-  float h[V];
   const float* first = cut.S > 1 ? cut.init : k.h0;
-#pragma unroll
-  for (int v = 0; v < V; ++v) h[v] = first ? first[p.j + v] : 0.0f;
-  Cols<E, V> z[U] = {}, x[U] = {};
+  float h = first != nullptr ? first[p.j] : 0.0f;
+  E z[U] = {}, x[U] = {};
+  // Loads without conditions, steps behind the last that is live in any lane from that
+  // one: in a branch of its own each load would be waited for before the next is sent.
+  const int32_t stop = (k.lens == nullptr ? end : wave_max(live > begin ? live : begin + 1)) - 1;
   const auto fetch = [&](int32_t t0) {
+    if (t0 >= end) return;
+    const int32_t from = t0 < stop ? t0 : stop;
+    auto rz = pz.row(from), rx = px.row(from);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (t0 + u < live) {
-        z[u] = load_cols<E, V>(pz + (t0 + u) * sz);
-        x[u] = load_cols<E, V>(px + (t0 + u) * sx);
-      }
+    for (int u = 0; u < U; ++u) {
+      z[u] = pz.in(rz);
+      x[u] = px.in(rx);
+      const bool more = t0 + u < stop;
+      rz += more ? pz.step : 0;
+      rx += more ? px.step : 0;
+    }
   };
   fetch(begin + w * U);
-  // every wave has its first state before one of them can write hT over it
-#pragma unroll
-  for (int v = 0; v < V; ++v) asm volatile("" : "+v"(h[v]));
-  for (int q = 0; q < s; ++q)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float2 m = cut.sums[q * (k.B * k.H) + p.j + v];
-      h[v] = m.x * h[v] + m.y;
-    }
+  asm volatile("" : "+v"(h));  // every wave has its first state before one can write hT over it
+  for (int q = 0; q < s; ++q) {
+    const float2 m = cut.sums[q * N + p.j];
+    h = fmaf(m.x, h, m.y);
+  }
 
   int phase = 0;
   for (int32_t t0 = begin; t0 < end; t0 += NW * U) {
     const int32_t t = t0 + w * U;
-    float a[U][V], q[U][V];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float c;
-        gate(load_as_f32(&z[u].v[v]), a[u][v], c);
-        const float xv = load_as_f32(&x[u].v[v]);
-        q[u][v] = COUPLED ? c * xv : xv;
-        if (t + u >= live) {
-          a[u][v] = 1.0f;
-          q[u][v] = 0.0f;
-        }
-      }
-    fetch(t + NW * U);
-    float now[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) now[v] = h[v];
-    if (NW > 1) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float A = a[0][v], Q = q[0][v];
-#pragma unroll
-        for (int u = 1; u < U; ++u) {
-          Q = a[u][v] * Q + q[u][v];
-          A *= a[u][v];
-        }
-        sums[phase][w][lane * V + v] = make_float2(A, Q);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < NW; ++i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (i == w) now[v] = h[v];
-          const float2 m = sums[phase][i][lane * V + v];
-          h[v] = m.x * h[v] + m.y;
-        }
-      phase ^= 1;
-    }
+    float a[U], q[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      Cols<E, V> o;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        now[v] = a[u][v] * now[v] + q[u][v];
-        o.v[v] = store_cast<E>(t + u < n ? now[v] : 0.0f);
-      }
-      if (p.on && t + u < end) *reinterpret_cast<Cols<E, V>*>(ph + (t + u) * sh) = o;
+      float c;
+      gate(load_as_f32(&z[u]), a[u], c);
+      const float xv = load_as_f32(&x[u]);
+      q[u] = COUPLED ? c * xv : xv;
     }
-    if (NW == 1)
+    const bool whole = k.lens == nullptr && t + U <= end;  // every step of the thread is live
+    if (!whole)
 #pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = now[v];
+      for (int u = 0; u < U; ++u)
+        if (t + u >= live) {
+          a[u] = 1.0f;
+          q[u] = 0.0f;
+        }
+    fetch(t + NW * U);
+    float now = h;
+    if (MODE == SHARED) {
+      float A = a[0], Q = q[0];
+#pragma unroll
+      for (int u = 1; u < U; ++u) {
+        Q = a[u] * Q + q[u];
+        A *= a[u];
+      }
+      sums[phase][w][lane] = make_float2(A, Q);
+      __syncthreads();
+      float Aw = 1.0f, Qw = 0.0f;  // the maps of the waves before this one, and of all
+      A = 1.0f;
+      Q = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        if (i == w) {
+          Aw = A;
+          Qw = Q;
+        }
+        const float2 m = sums[phase][i][lane];
+        Q = fmaf(m.x, Q, m.y);
+        A *= m.x;
+      }
+      now = fmaf(Aw, h, Qw);
+      h = fmaf(A, h, Q);
+      phase ^= 1;
+    }
+    auto rh = ph.row(t);
+    if (whole && p.on) {
+#pragma unroll
+      for (int u = 0; u < U; ++u, rh += ph.step) {
+        now = a[u] * now + q[u];
+        ph.in(rh) = store_cast<E>(now);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u, rh += ph.step) {
+        now = a[u] * now + q[u];
+        if (p.on && t + u < end) ph.in(rh) = store_cast<E>(t + u < n ? now : 0.0f);
+      }
+    }
+    if (MODE == ALONE) h = now;
   }
-  if (k.hT != nullptr && p.on && s == cut.S - 1 && w == 0)
-#pragma unroll
-    for (int v = 0; v < V; ++v) k.hT[p.j + v] = h[v];
+  if (k.hT != nullptr && p.on && w == 0 && end == T) k.hT[p.j] = h;
 }
 
 // ---------------------------------------------------------------------------
 // Gradient, from the last step backwards. The states before a thread's eight steps are
 // recomputed from the one before the first of them, the only row of hs that it reads.
 // ---------------------------------------------------------------------------
-template <typename E, bool COUPLED, int V, int NW>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_gated_scan_grad_kernel(GatedScan k, Cut cut) {
-  constexpr int U = kUnroll;
-  __shared__ float2 sums[2][NW == 1 ? 1 : NW][NW == 1 ? 1 : 64 * V];
+template <typename E, bool COUPLED, int MODE>
+__global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_scan_grad_kernel(GatedScan k, Cut cut) {
+  constexpr int U = kUnroll, NW = MODE == ALONE ? 1 : kWaves;
+  __shared__ float2 sums[2][NW][MODE == ALONE ? 1 : 64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  const int w = NW == 1 ? 0 : wave;
-  const int s = static_cast<int>(blockIdx.x) / cut.tiles;
+  const int w = MODE == ALONE ? 0 : wave;
   const int block = static_cast<int>(blockIdx.x) % cut.tiles;
-  const Place p = place_of<V>(NW == 1 ? block * 4 + wave : block, lane, k);
-  if (NW == 1 && !p.on) return;
+  const int s = static_cast<int>(blockIdx.x) / cut.tiles;
+  const Place p = place_of(MODE == ALONE ? block * 4 + wave : block, lane, k);
+  if (MODE == ALONE && !p.on) return;
+  const int64_t N = k.B * k.H;
+  const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;
-  const int32_t end = k.T - begin < cut.len ? static_cast<int32_t>(k.T) : begin + cut.len;
+  const int32_t end = T - begin < cut.len ? T : begin + cut.len;
+  const int32_t last = begin + (end - begin - 1) / (NW * U) * (NW * U);  // first step of the last block
   const int32_t n = length_of(k.lens, p.b, k.T);
   const int32_t live = !p.on ? 0 : n < end ? n : end;
-  const E* pz = static_cast<const E*>(k.z) + p.b * k.ldz + p.c;
-  const E* px = static_cast<const E*>(k.x) + p.b * k.ldx + p.c;
-  const E* ph = static_cast<const E*>(k.hs) + p.b * k.ldh + p.c;
-  const E* pd = static_cast<const E*>(k.dhs) + p.b * k.lddh + p.c;
-  E* gz = static_cast<E*>(k.dz) + p.b * k.lddz + p.c;
-  E* gx = static_cast<E*>(k.dx) + p.b * k.lddx + p.c;
-  const int64_t sz = k.B * k.ldz, sx = k.B * k.ldx, sh = k.B * k.ldh, sd = k.B * k.lddh;
-  const int64_t tz = k.B * k.lddz, tx = k.B * k.lddx;
   const bool has_d = k.dhs != nullptr;
+  const Rows<E> pz(k.z, k.ldz, k.B, p), px(k.x, k.ldx, k.B, p), ph(k.hs, k.ldh, k.B, p);
+  const Rows<E> pd(has_d ? k.dhs : k.z, has_d ? k.lddh : k.ldz, k.B, p);
+  const Rows<E> gz(k.dz, k.lddz, k.B, p), gx(k.dx, k.lddx, k.B, p);
 
-  float mu[V];
   const float* first = cut.S > 1 ? cut.init : k.dhT;
-#pragma unroll
-  for (int v = 0; v < V; ++v) mu[v] = first ? first[p.j + v] : 0.0f;
-  Cols<E, V> z[U] = {}, x[U] = {}, d[U] = {}, before = {};
-  const auto fetch = [&](int32_t t0) {
+  float mu = first != nullptr ? first[p.j] : 0.0f;
+  E z[U] = {}, x[U] = {}, d[U] = {}, before = {};
+  const int32_t stop = (k.lens == nullptr ? end : wave_max(live > begin ? live : begin + 1)) - 1;
+  const auto fetch = [&](int32_t t0) {  // as in the forward call
     if (t0 < begin) return;
+    const int32_t from = t0 < stop ? t0 : stop;
+    auto rz = pz.row(from), rx = px.row(from), rd = pd.row(from);
+    before = ph.in(ph.row(from > 0 ? from - 1 : 0));
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (t0 + u < live) {
-        z[u] = load_cols<E, V>(pz + (t0 + u) * sz);
-        x[u] = load_cols<E, V>(px + (t0 + u) * sx);
-        if (has_d) d[u] = load_cols<E, V>(pd + (t0 + u) * sd);
-      }
-    if (t0 > 0 && t0 < live) before = load_cols<E, V>(ph + (t0 - 1) * sh);
-  };
-  const int32_t last = begin + (end - begin - 1) / (NW * U) * (NW * U);
-  fetch(last + w * U);
-  // every wave has its adjoint before one of them can write dh0 over it
-#pragma unroll
-  for (int v = 0; v < V; ++v) asm volatile("" : "+v"(mu[v]));
-  for (int q = cut.S - 1; q > s; --q)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float2 m = cut.sums[q * (k.B * k.H) + p.j + v];
-      mu[v] = m.x * mu[v] + m.y;
+    for (int u = 0; u < U; ++u) {
+      z[u] = pz.in(rz);
+      x[u] = px.in(rx);
+      d[u] = pd.in(rd);
+      const bool more = t0 + u < stop;
+      rz += more ? pz.step : 0;
+      rx += more ? px.step : 0;
+      rd += more ? pd.step : 0;
     }
+  };
+  fetch(last + w * U);
+  asm volatile("" : "+v"(mu));  // every wave has its adjoint before one can write dh0 over it
+  for (int q = cut.S - 1; q > s; --q) {
+    const float2 m = cut.sums[q * N + p.j];
+    mu = fmaf(m.x, mu, m.y);
+  }
 
   int phase = 0;
   for (int32_t t0 = last; t0 >= begin; t0 -= NW * U) {
     const int32_t t = t0 + w * U;
-    float a[U][V], c[U][V], xs[U][V], hp[U][V], dh[U][V];
+    float a[U], c[U], xs[U], hp[U], dh[U];
+    hp[0] = t > 0 ? load_as_f32(&before) : k.h0 != nullptr ? k.h0[p.j] : 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      hp[0][v] = t > 0 ? load_as_f32(&before.v[v]) : k.h0 ? k.h0[p.j + v] : 0.0f;
+    for (int u = 0; u < U; ++u) {
+      gate(load_as_f32(&z[u]), a[u], c[u]);
+      xs[u] = load_as_f32(&x[u]);
+      dh[u] = load_as_f32(&d[u]);
+      if (u + 1 < U) hp[u + 1] = a[u] * hp[u] + (COUPLED ? c[u] * xs[u] : xs[u]);
+    }
+    const bool whole = k.lens == nullptr && has_d && t + U <= end;  // every step is live
+    if (!whole)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        gate(load_as_f32(&z[u].v[v]), a[u][v], c[u][v]);
-        xs[u][v] = load_as_f32(&x[u].v[v]);
-        dh[u][v] = has_d ? load_as_f32(&d[u].v[v]) : 0.0f;
-        if (t + u >= live) {
-          a[u][v] = 1.0f;
-          dh[u][v] = 0.0f;
-        }
-        if (u + 1 < U) hp[u + 1][v] = a[u][v] * hp[u][v] + (COUPLED ? c[u][v] * xs[u][v] : xs[u][v]);
+      for (int u = 0; u < U; ++u) {
+        if (t + u >= live) a[u] = 1.0f;
+        if (t + u >= live || !has_d) dh[u] = 0.0f;
       }
     fetch(t - NW * U);
-    float now[V];
+    float now = mu;
+    if (MODE == SHARED) {
+      float A = 1.0f, M = 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) now[v] = mu[v];
-    if (NW > 1) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float A = 1.0f, M = 0.0f;
-#pragma unroll
-        for (int u = U - 1; u >= 0; --u) {
-          M = a[u][v] * (M + dh[u][v]);
-          A *= a[u][v];
-        }
-        sums[phase][w][lane * V + v] = make_float2(A, M);
+      for (int u = U - 1; u >= 0; --u) {
+        M = a[u] * (M + dh[u]);
+        A *= a[u];
       }
+      sums[phase][w][lane] = make_float2(A, M);
       __syncthreads();
+      float Aw = 1.0f, Mw = 0.0f;  // the maps of the waves after this one, and of all
+      A = 1.0f;
+      M = 0.0f;
 #pragma unroll
-      for (int i = NW - 1; i >= 0; --i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (i == w) now[v] = mu[v];
-          const float2 m = sums[phase][i][lane * V + v];
-          mu[v] = m.x * mu[v] + m.y;
+      for (int i = NW - 1; i >= 0; --i) {
+        if (i == w) {
+          Aw = A;
+          Mw = M;
         }
+        const float2 m = sums[phase][i][lane];
+        M = fmaf(m.x, M, m.y);
+        A *= m.x;
+      }
+      now = fmaf(Aw, mu, Mw);
+      mu = fmaf(A, mu, M);
       phase ^= 1;
     }
+    auto rz = gz.row(t + U - 1), rx = gx.row(t + U - 1);
+    if (whole && p.on) {
 #pragma unroll
-    for (int u = U - 1; u >= 0; --u) {
-      Cols<E, V> oz, ox;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float lam = now[v] + dh[u][v];
-        const float prev = COUPLED ? hp[u][v] - xs[u][v] : hp[u][v];
-        const bool in = t + u < live;
-        oz.v[v] = store_cast<E>(in ? lam * prev * (a[u][v] * c[u][v]) : 0.0f);
-        ox.v[v] = store_cast<E>(in ? (COUPLED ? c[u][v] * lam : lam) : 0.0f);
-        now[v] = a[u][v] * lam;
+      for (int u = U - 1; u >= 0; --u, rz -= gz.step, rx -= gx.step) {
+        const float lam = now + dh[u];
+        now = a[u] * lam;
+        gz.in(rz) = store_cast<E>((COUPLED ? hp[u] - xs[u] : hp[u]) * c[u] * now);
+        gx.in(rx) = store_cast<E>(COUPLED ? c[u] * lam : lam);
       }
-      if (p.on && t + u < end) {
-        *reinterpret_cast<Cols<E, V>*>(gz + (t + u) * tz) = oz;
-        *reinterpret_cast<Cols<E, V>*>(gx + (t + u) * tx) = ox;
+    } else {
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u, rz -= gz.step, rx -= gx.step) {
+        const float lam = now + dh[u];
+        now = a[u] * lam;
+        const bool in = t + u < live;
+        if (p.on && t + u < end) {
+          gz.in(rz) = store_cast<E>(in ? (COUPLED ? hp[u] - xs[u] : hp[u]) * c[u] * now : 0.0f);
+          gx.in(rx) = store_cast<E>(in ? (COUPLED ? c[u] * lam : lam) : 0.0f);
+        }
       }
     }
-    if (NW == 1)
-#pragma unroll
-      for (int v = 0; v < V; ++v) mu[v] = now[v];
+    if (MODE == ALONE) mu = now;
   }
-  if (k.dh0 != nullptr && p.on && s == 0 && w == 0)
-#pragma unroll
-    for (int v = 0; v < V; ++v) k.dh0[p.j + v] = mu[v];
+  if (k.dh0 != nullptr && p.on && w == 0 && begin == 0) k.dh0[p.j] = mu;
 }
 
 // ---------------------------------------------------------------------------
-// What each segment does to its states (one column a lane): the waves take equal
-// stretches of it, whose sums are composed in order. ADJOINT: of the gradient, backwards
-// (the stretches are read forwards, the last wave's applied first).
+// The map of each segment: the waves take equal stretches of it, whose maps are composed
+// in order. ADJOINT: of the gradient, backwards in time (the stretches are read
+// forwards, the last wave's applied first).
 // ---------------------------------------------------------------------------
 template <typename E, bool COUPLED, bool ADJOINT>
 __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(GatedScan k, Cut cut) {
@@ -325,49 +355,51 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
   __shared__ float2 sums[kWaves][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  // the forward call needs no sum of the last segment, the gradient none of the first
+  // the forward call needs no map of the last segment, the gradient none of the first
   const int s = static_cast<int>(blockIdx.x) / cut.tiles + (ADJOINT ? 1 : 0);
-  const Place p = place_of<1>(static_cast<int>(blockIdx.x) % cut.tiles, lane, k);
+  const Place p = place_of(static_cast<int>(blockIdx.x) % cut.tiles, lane, k);
+  const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;
-  const int32_t end = k.T - begin < cut.len ? static_cast<int32_t>(k.T) : begin + cut.len;
+  const int32_t end = T - begin < cut.len ? T : begin + cut.len;
   const int32_t n = length_of(k.lens, p.b, k.T);
-  const int32_t live = !p.on ? 0 : n < end ? n : end;
-  const E* pz = static_cast<const E*>(k.z) + p.b * k.ldz + p.c;
-  const int64_t sz = k.B * k.ldz;
-  const E* pu = ADJOINT ? static_cast<const E*>(k.dhs) + p.b * k.lddh + p.c
-                        : static_cast<const E*>(k.x) + p.b * k.ldx + p.c;
-  const int64_t su = ADJOINT ? k.B * k.lddh : k.B * k.ldx;
-  const bool has_u = ADJOINT ? k.dhs != nullptr : true;
+  const bool has_u = !ADJOINT || k.dhs != nullptr;
+  const Rows<E> pz(k.z, k.ldz, k.B, p);
+  const Rows<E> pu(!ADJOINT ? k.x : has_u ? k.dhs : k.z, !ADJOINT ? k.ldx : has_u ? k.lddh : k.ldz, k.B, p);
   if (p.on && wave == 0 && s == (ADJOINT ? cut.S - 1 : 0)) {
     const float* first = ADJOINT ? k.dhT : k.h0;
-    cut.init[p.j] = first ? first[p.j] : 0.0f;
+    cut.init[p.j] = first != nullptr ? first[p.j] : 0.0f;
   }
 
   const int32_t stretch = (cut.len + kWaves * U - 1) / (kWaves * U) * U;
-  const int32_t t_end = begin + (wave + 1) * stretch < end ? begin + (wave + 1) * stretch : end;
+  const int32_t t_begin = begin + wave * stretch;
+  const int32_t t_end = t_begin + stretch < end ? t_begin + stretch : end;
+  const int32_t live = !p.on ? 0 : n < t_end ? n : t_end;
+  const int32_t t_live = k.lens == nullptr ? t_end : wave_max(live);  // no step is live in any lane beyond
   float A = 1.0f, Q = 0.0f;
-  for (int32_t t0 = begin + wave * stretch; t0 < t_end; t0 += U) {
-    E z[U] = {}, v[U] = {};
+  for (int32_t t0 = t_begin; t0 < t_live; t0 += U) {
+    E z[U], v[U];
+    auto rz = pz.row(t0), ru = pu.row(t0);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (t0 + u < live && t0 + u < t_end) {
-        z[u] = pz[(t0 + u) * sz];
-        if (has_u) v[u] = pu[(t0 + u) * su];
-      }
+    for (int u = 0; u < U; ++u) {
+      z[u] = pz.in(rz);
+      v[u] = pu.in(ru);
+      const bool more = t0 + u + 1 < t_live;
+      rz += more ? pz.step : 0;
+      ru += more ? pu.step : 0;
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float a, c;
       gate(load_as_f32(&z[u]), a, c);
       float q = has_u ? load_as_f32(&v[u]) : 0.0f;
-      const bool in = t0 + u < live && t0 + u < t_end;
+      const bool in = t0 + u < live;
       if (ADJOINT) {
-        // mu -> A mu + Q before this earlier stretch of steps, step t after: A' = A a, and its
-        // own dh reaches through a and all steps before it
+        // the adjoint of step t reaches the state before the stretch through the gates up to its own
         A = in ? A * a : A;
-        Q = in ? Q + A * q : Q;
+        Q = in ? fmaf(A, q, Q) : Q;
       } else {
         q = COUPLED ? c * q : q;
-        Q = in ? a * Q + q : Q;
+        Q = in ? fmaf(a, Q, q) : Q;
         A = in ? A * a : A;
       }
     }
@@ -379,85 +411,59 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
       const float2 o = sums[ADJOINT ? kWaves - 1 - i : i][lane];
-      m = make_float2(o.x * m.x, o.x * m.y + o.y);
+      m = make_float2(o.x * m.x, fmaf(o.x, m.y, o.y));
     }
     cut.sums[s * (k.B * k.H) + p.j] = m;
   }
 }
 
 // ---------------------------------------------------------------------------
-// Choice of the variant.
+// Choice of the variant, for N states: alone where a thread to each state fills the GPU
+// (sixteen waves on a compute unit) or there are no steps to share; in segments where the
+// tiles of states are so few that the second reading costs less than the idle units:
+// T 4096, 128 tiles of bf16, forward and gradient 267 us in one piece, 176 in four segments;
+// T 777, 204 tiles of float32, 85-91 in one piece, 92 in three.
 // ---------------------------------------------------------------------------
-constexpr int64_t kBlocks = 512;       // workgroups that fill the GPU: two on a compute unit
+constexpr int64_t kBlocks = 512;       // two workgroups on a compute unit
+constexpr int64_t kUncut = 192;        // tiles from which the second reading costs more than it gives
 constexpr int32_t kShortest = 128;     // steps of a segment at least
 
-// Segments of a call of N states, and the steps of one.
+bool alone(int64_t T, int64_t N) { return T <= 2 * kUnroll || (N + 63) / 64 >= 4096; }
+
+// Segments of a call, and the steps of one.
 int segments(int64_t T, int64_t N, int32_t* len) {
-  const int64_t tiles = (N + 63) / 64;
-  int64_t S = tiles >= kBlocks ? 1 : (kBlocks + tiles - 1) / tiles;
+  const int64_t tiles = (N + 63) / 64, step = kWaves * kUnroll;
+  int64_t S = alone(T, N) || tiles >= kUncut ? 1 : (kBlocks + tiles - 1) / tiles;
   if (S > T / kShortest) S = T / kShortest;
   if (S < 1) S = 1;
-  const int64_t step = int64_t(kWaves) * kUnroll;
-  int64_t L = S == 1 ? T : ((T + S - 1) / S + step - 1) / step * step;
+  const int64_t L = S == 1 ? T : ((T + S - 1) / S + step - 1) / step * step;
   *len = static_cast<int32_t>(L);
   return static_cast<int>((T + L - 1) / L);
-}
-
-struct Variant {
-  int V;
-  bool alone;  // a thread takes its states through all steps
-};
-// Widest vectors that rows and columns allow, as long as the states fill the GPU: with
-// two waves on every SIMD when a thread goes alone, with two workgroups to a compute unit
-// when waves share the steps. Few steps leave nothing to share.
-Variant variant(const GatedScan& c, bool cut, int widest) {
-  const int64_t N = c.B * c.H;
-  int V = widest;
-  const int64_t lds[] = {c.H, c.ldz, c.ldx, c.ldh, c.dhs ? c.lddh : 0, c.dz ? c.lddz : 0, c.dx ? c.lddx : 0};
-  for (const int64_t ld : lds)
-    while (ld % V != 0) V /= 2;
-  const auto waves = [&](int v) { return (N + 64 * v - 1) / (64 * v); };
-  if (cut) return Variant{1, false};
-  if (c.T <= 2 * kUnroll || waves(1) >= 8192) {
-    while (V > 1 && waves(V) < 2048) V /= 2;
-    return Variant{V, true};
-  }
-  while (V > 1 && waves(V) < kBlocks) V /= 2;
-  return Variant{V, false};
 }
 
 template <typename E, bool COUPLED, bool GRAD>
 hipError_t run(const GatedScan& c, void* ws, hipStream_t s) {
   const int64_t N = c.B * c.H;
-  Cut cut{};
-  cut.S = 1;
-  cut.len = static_cast<int32_t>(c.T);
+  Cut cut{1, static_cast<int32_t>(c.T), static_cast<int>((N + 63) / 64), nullptr, nullptr};
+  if (alone(c.T, N)) {
+    cut.tiles = (cut.tiles + 3) / 4;
+    if constexpr (GRAD)
+      launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, ALONE>, dim3(cut.tiles), dim3(256), s, c, cut);
+    else
+      launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, ALONE>, dim3(cut.tiles), dim3(256), s, c, cut);
+    return hipGetLastError();
+  }
+  const dim3 block(64 * kWaves);
   if (ws != nullptr) cut.S = segments(c.T, N, &cut.len);
-  const Variant v = variant(c, cut.S > 1, GRAD ? 2 : 4);
-  const int64_t waves = (N + 64 * v.V - 1) / (64 * v.V);
-  cut.tiles = static_cast<int>(v.alone ? (waves + 3) / 4 : waves);
   if (cut.S > 1) {
     cut.init = static_cast<float*>(ws);
     cut.sums = reinterpret_cast<float2*>(cut.init + (N + 63) / 64 * 64);
-    launch_kernel(dlvm_gated_scan_sums_kernel<E, COUPLED, GRAD>, dim3(cut.tiles * (cut.S - 1)),
-                  dim3(64 * kWaves), s, c, cut);
+    launch_kernel(dlvm_gated_scan_sums_kernel<E, COUPLED, GRAD>, dim3(cut.tiles * (cut.S - 1)), block, s, c, cut);
   }
-  const dim3 grid(static_cast<uint32_t>(cut.tiles) * cut.S), block(v.alone ? 256 : 64 * kWaves);
-  if constexpr (GRAD) {
-    auto f = v.V == 2 ? (v.alone ? dlvm_gated_scan_grad_kernel<E, COUPLED, 2, 1>
-                                 : dlvm_gated_scan_grad_kernel<E, COUPLED, 2, kWaves>)
-                      : (v.alone ? dlvm_gated_scan_grad_kernel<E, COUPLED, 1, 1>
-                                 : dlvm_gated_scan_grad_kernel<E, COUPLED, 1, kWaves>);
-    launch_kernel(f, grid, block, s, c, cut);
-  } else {
-    auto f = v.V == 4   ? (v.alone ? dlvm_gated_scan_kernel<E, COUPLED, 4, 1>
-                                   : dlvm_gated_scan_kernel<E, COUPLED, 4, kWaves>)
-             : v.V == 2 ? (v.alone ? dlvm_gated_scan_kernel<E, COUPLED, 2, 1>
-                                   : dlvm_gated_scan_kernel<E, COUPLED, 2, kWaves>)
-                        : (v.alone ? dlvm_gated_scan_kernel<E, COUPLED, 1, 1>
-                                   : dlvm_gated_scan_kernel<E, COUPLED, 1, kWaves>);
-    launch_kernel(f, grid, block, s, c, cut);
-  }
+  if constexpr (GRAD)
+    launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, SHARED>, dim3(cut.tiles * cut.S), block, s, c, cut);
+  else
+    launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, SHARED>, dim3(cut.tiles * cut.S), block, s, c, cut);
   return hipGetLastError();
 }
 
