@@ -1,6 +1,20 @@
 // Scores of tokens under rows of logits: log probabilities of given tokens,
 // log-sum-exp, entropy and the largest alternatives, and the gradient of the log
 // probabilities and the entropy.
+//
+// The scores are taken in one pass over the logits. Each thread keeps the running
+// maximum m of its logits and the sums s = sum 2^t and w = sum 2^t t, t the distance of
+// scale z log2(e) from that maximum; they are rescaled once for every 16 or 32 logits, when a
+// new maximum is known. The entropy is log s - w / s: all terms of w have one sign, so it
+// has no cancellation beyond its own size. Alternatives are collected in the same pass:
+// from the first tile of a row comes a bound that at least `top` logits reach (the
+// top-th largest of 64 maxima of disjoint parts of it), and the few logits that reach it are
+// kept in LDS, in lists of the waves that are cut back to the `top` best when full. So the
+// common logit costs one comparison for eight, and any order of logits is right.
+// A row is a wave's where it is short, else a workgroup's; with a workspace, a call of few
+// rows cuts them into parts, joined by a second launch.
+// bf16 logits are bound by both memory and arithmetic (about ten operations for two
+// bytes, the exponential four of them), float32 ones by memory.
 #include <math.h>
 
 #include "common.hpp"
@@ -12,6 +26,11 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
+// Up to this size scale z log2(e) is taken in one operation from a maximum rounded
+// after the product (whose rounding is accounted for); beyond, from differences of the
+// logits themselves: the rounding of a product the size of the type's lowest value is
+// larger than any exponent.
+constexpr float kPlain = 16384.0f;
 
 // The order of alternatives as whole numbers: greater is better. NaN counts as
 // -infinity and -0 as 0; among equal logits the lower class is greater.
@@ -29,144 +48,604 @@ __device__ __forceinline__ uint32_t key_class(uint64_t key) {
   return 0xffffffffu - static_cast<uint32_t>(key);
 }
 
-// A part of a row: the maximum m of its logits and, with y = (z - m) scale log2(e)
-// (differences of the logits themselves: a product rounded before the subtraction is
-// off by as much as the exponent where logits are as large as the type's lowest value),
-// s = sum 2^y and w = sum 2^y y. All terms of w have one sign, so that the entropy
-// log s - w / s has no cancellation beyond its own size. y is clamped to a finite
-// value where a class is masked, so that its term is 0 and not 0 times infinity.
+__device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float log2_(float v) { return __builtin_amdgcn_logf(v); }
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ int bits_below(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32),
+                                   __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
+}
+
+// Of a set of logits: their maximum m and, with t = (z - m) scale log2(e) + r, s = sum 2^t
+// and w = sum 2^t t. (r: what a maximum rounded after its product is off by; 0 once the set is
+// complete.)
 struct Part {
   float m, s, w;
 };
+
 // Nothing left: every class is masked, by -infinity or by the type's lowest value.
 __device__ __forceinline__ bool masked_everywhere(const Part& p, float scale) {
   return p.s == 0.0f || (p.s == p.s && p.m * scale < -1e30f);
 }
-__device__ __forceinline__ float below(float z, float m, float c2) {
-  return fmaxf((z - m) * c2, -1e30f);
+
+// p moved to the maximum m >= p.m, d = (p.m - m) scale log2(e) - r. (Nothing to move where
+// the set is empty, whose d may be infinite.)
+__device__ __forceinline__ void move_to(Part& p, float m, float d) {
+  const float e = exp2_(d);
+  p.w = p.s == 0.0f ? 0.0f : (p.w + p.s * d) * e;
+  p.s = p.s == 0.0f ? 0.0f : p.s * e;
+  p.m = m;
 }
-__device__ __forceinline__ Part join(const Part& a, const Part& b, float c2) {
-  const float m = fmaxf(a.m, b.m);
-  Part r{m, 0.0f, 0.0f};
-  if (a.s != 0.0f) {
-    const float d = below(a.m, m, c2), e = exp2f(d);
-    r.s += a.s * e;
-    r.w += (a.w + d * a.s) * e;
+
+template <typename T> struct Vec;
+template <> struct Vec<bf16_t> {
+  static constexpr int N = 8;
+  struct __attribute__((packed, aligned(2))) Raw { uint32_t w[4]; } raw;
+  __device__ __forceinline__ float operator[](int i) const {
+    return __uint_as_float(i % 2 == 0 ? raw.w[i / 2] << 16 : raw.w[i / 2] & 0xffff0000u);
   }
-  if (b.s != 0.0f) {
-    const float d = below(b.m, m, c2), e = exp2f(d);
-    r.s += b.s * e;
-    r.w += (b.w + d * b.s) * e;
+};
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  struct __attribute__((packed, aligned(4))) Raw { uint32_t w[4]; } raw;
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(raw.w[i]); }
+};
+
+// ---------------------------------------------------------------------------
+// Alternatives. The list of a wave: keys in LDS, no more than kList; `tau` is the greatest
+// key that is not wanted any more, `bound` the least logit that may be wanted. (A wave's
+// row of up to kList classes fits whole.)
+// ---------------------------------------------------------------------------
+constexpr int kList = 256;
+
+struct Wanted {
+  uint64_t tau;
+  float bound;
+  int n;
+};
+
+// Cuts the list back to its `top` best, in order.
+__device__ __forceinline__ void cut_back(volatile uint64_t* list, Wanted& f, int top) {
+  const int lane = threadIdx.x & 63;
+  uint64_t mine[kList / 64];
+  int rank[kList / 64];
+#pragma unroll
+  for (int i = 0; i < kList / 64; ++i) {
+    mine[i] = lane + 64 * i < f.n ? list[lane + 64 * i] : 0;
+    rank[i] = 0;
   }
-  return r;
+#pragma unroll 1
+  for (int j = 0; j < f.n; ++j) {
+    const uint64_t other = list[j];
+#pragma unroll
+    for (int i = 0; i < kList / 64; ++i) rank[i] += other > mine[i];
+  }
+#pragma unroll
+  for (int i = 0; i < kList / 64; ++i)
+    if (lane + 64 * i < f.n && rank[i] < top) list[rank[i]] = mine[i];
+  if (f.n >= top) {
+    f.n = top;
+    const uint64_t last = list[top - 1];
+    const uint32_t high = __builtin_amdgcn_readfirstlane(static_cast<int>(last >> 32));
+    const uint32_t low = __builtin_amdgcn_readfirstlane(static_cast<int>(last));
+    f.tau = static_cast<uint64_t>(high) << 32 | low;
+    f.bound = key_logit(f.tau);
+  }
+}
+
+// One logit of each lane at the end of the list, as far as there is room; counted all the same.
+__device__ __forceinline__ void append(volatile uint64_t* list, Wanted& f, float z, uint32_t c, bool valid) {
+  const uint64_t key = rank_key(z, c);
+  const bool wanted = valid && key > f.tau;
+  const uint64_t take = __ballot(wanted);
+  const int at = f.n + bits_below(take);
+  if (wanted && at < kList) list[at] = key;
+  f.n += __builtin_popcountll(take);
+}
+
+// The logits of one tile, class c0 + i of each lane's U vectors of N, 64 classes at a time with
+// room made before each: for the tile that would overflow the list. It reads them again.
+template <typename T, int N, int U>
+__device__ __forceinline__ void append_carefully(volatile uint64_t* list, Wanted& f, int top, const T* z,
+                                                 int64_t c0, int64_t stride, int64_t c1) {
+#pragma unroll 1
+  for (int i = 0; i < U * N; ++i) {
+    const int64_t c = c0 + (i / N) * stride + i % N;
+    const bool valid = c < c1;
+    const float v = valid ? load_as_f32(z + c) : 0.0f;
+    if (f.n + 64 > kList) cut_back(list, f, top);
+    append(list, f, v, static_cast<uint32_t>(c), valid);
+  }
+}
+
+// A logit that at least `top` of 64 values reach: the top-th largest of them.
+__device__ __forceinline__ float reached_by(const float* values, int top) {
+  const float v = values[threadIdx.x & 63];
+  int greater = 0;
+  for (int i = 0; i < 64; i += 4) {
+    const float4 o = *reinterpret_cast<const float4*>(values + i);
+    greater += (o.x > v) + (o.y > v) + (o.z > v) + (o.w > v);
+  }
+  return -wave_max(greater < top ? -v : -INFINITY);
+}
+
+// ---------------------------------------------------------------------------
+// Scores. NW waves share a row (or a part of one); NW = 1: four rows to a workgroup.
+// ---------------------------------------------------------------------------
+constexpr int kRowWaves = 8;
+constexpr int kUnroll = 4;  // vectors of a thread in flight
+
+struct Cut {
+  int parts;          // of a row (1: whole rows)
+  int64_t len;        // classes of a part
+  Part* stats;        // [rows * parts]
+  uint64_t* keys;     // [rows * parts][top], falling, 0 where a part has fewer
+};
+
+// The scores of a row from its complete sums; z is the token's logit.
+__device__ __forceinline__ void write_scores(const TokenScores& k, int64_t row, const Part& p, float log_s,
+                                             bool masked, float z) {
+  if (k.lse != nullptr) k.lse[row] = masked ? -INFINITY : p.m * k.scale + log_s;
+  if (k.entropy != nullptr) k.entropy[row] = masked ? 0.0f : log_s - p.w / p.s * kLn2;
+  if (k.logp != nullptr) {
+    const int32_t t = k.tokens[row];
+    k.logp[row] = t == -1                     ? 0.0f
+                  : t < 0 || t >= k.classes   ? NAN
+                  : masked                    ? -INFINITY
+                                              : (z - p.m) * k.scale - log_s;
+  }
+}
+__device__ __forceinline__ void write_top(const TokenScores& k, int64_t row, int rank, uint64_t key,
+                                          const Part& p, float log_s, bool masked) {
+  k.top_ids[row * k.top + rank] = static_cast<int32_t>(key_class(key));
+  k.top_logp[row * k.top + rank] = masked ? -INFINITY : (key_logit(key) - p.m) * k.scale - log_s;
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void dlvm_token_scores_kernel(TokenScores k) {
-  __shared__ Part parts[256];
-  __shared__ uint64_t best[256];
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const int64_t V = k.classes;
+__device__ __forceinline__ float token_logit(const TokenScores& k, int64_t row) {
+  if (k.tokens == nullptr) return 0.0f;
+  const int32_t t = k.tokens[row];
+  return t >= 0 && t < k.classes ? load_as_f32(static_cast<const T*>(k.logits) + row * k.ld + t) : 0.0f;
+}
+
+template <typename T, int NW, bool TOP, bool PARTS>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_kernel(TokenScores k, Cut cut) {
+  constexpr int N = Vec<T>::N, WAVES = NW == 1 ? 4 : NW, U = kUnroll;
+  constexpr int tile = 64 * NW * N * U;  // classes
+  __shared__ uint64_t lists[TOP ? WAVES : 1][TOP ? kList : 1];
+  __shared__ __align__(16) float heads[TOP ? (NW == 1 ? 4 : 1) : 1][64];
+  __shared__ float red[3][WAVES];
+  __shared__ int counts[WAVES];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+  const int tid = NW == 1 ? lane : threadIdx.x;
+  int64_t row = NW == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
+  int part = 0;
+  if (PARTS) {
+    part = static_cast<int>(blockIdx.x % static_cast<uint32_t>(cut.parts));
+    row = blockIdx.x / static_cast<uint32_t>(cut.parts);
+  }
+  if (row >= k.rows) return;  // only whole waves of NW = 1, which meet no barrier
   const T* z = static_cast<const T*>(k.logits) + row * k.ld;
+  const int64_t c0 = PARTS ? part * cut.len : 0;
+  const int64_t c1 = PARTS && c0 + cut.len < k.classes ? c0 + cut.len : k.classes;
   const float c2 = k.scale * kLog2e;
+  const float zt = !PARTS && tid == 0 ? token_logit<T>(k, row) : 0.0f;
+
   Part p{-INFINITY, 0.0f, 0.0f};
-  for (int64_t c = tid; c < V; c += 256) {
-    const float v = load_as_f32(z + c);
-    const Part one{v, v != v || v == INFINITY ? NAN : v == -INFINITY ? 0.0f : 1.0f, 0.0f};
-    p = join(p, one, c2);
+  float r = 0.0f;
+  Wanted f{0, -INFINITY, 0};
+  uint64_t* list = TOP ? lists[wave] : nullptr;
+
+  Vec<T> v[U];
+  // The vectors of the tile that starts at class `at`; behind the end of the row, elements of
+  // -infinity.
+  const auto load = [&](int64_t at) {
+    if (at + tile <= c1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(z + at + (u * 64 * NW + tid) * N);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t c = at + (u * 64 * NW + tid) * N;
+        if (c + N <= c1) {
+          v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(z + c);
+        } else {
+          constexpr int bits = 8 * sizeof(T);
+          constexpr uint32_t low = bits == 16 ? 0xff80u : 0xff800000u;  // -infinity
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[u].raw.w[i] = 0;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            uint32_t b = low;
+            if (c + i < c1) b = bits == 16 ? reinterpret_cast<const uint16_t*>(z)[c + i]
+                                           : reinterpret_cast<const uint32_t*>(z)[c + i];
+            v[u].raw.w[i * bits / 32] |= b << (i * bits % 32);
+          }
+        }
+      }
+    }
+  };
+
+  load(c0);
+  for (int64_t at = c0; at < c1; at += tile) {
+    float zs[U][N], top_of[U];
+    float big = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float b = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        zs[u][i] = v[u][i];
+        b = fmaxf(b, zs[u][i]);
+      }
+      top_of[u] = b;
+      big = fmaxf(big, b);
+    }
+    if (at + tile < c1) load(at + tile);
+
+    // the maximum so far, and the sums moved to it
+    const float m = fmaxf(p.m, big);
+    const float ref = m == -INFINITY ? 0.0f : m;  // nothing yet: any reference does
+    float M = ref * c2;
+    const bool plain = __all(fabsf(M) < kPlain) != 0;
+    const float r_new = plain ? fmaf(ref, c2, -M) : 0.0f;
+    move_to(p, m, (p.m - ref) * c2 + (r_new - r));
+    r = r_new;
+    if (plain) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float t = fmaf(zs[u][i], c2, -M);
+          const float e = exp2_(t);
+          p.s += e;
+          p.w = fmaf(e, fmaxf(t, -1e4f), p.w);  // a masked class: 0 times a finite number
+        }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float t = (zs[u][i] - ref) * c2;
+          const float e = exp2_(t);
+          p.s += e;
+          p.w = fmaf(e, fmaxf(t, -1e4f), p.w);
+        }
+    }
+
+    if (TOP) {
+      if (at == c0) {
+        float head = big;
+        if (NW > 1) {  // of eight threads, so that 64 heads cover the workgroup
+          head = fmaxf(head, __shfl_xor(head, 1, 64));
+          head = fmaxf(head, __shfl_xor(head, 2, 64));
+          head = fmaxf(head, __shfl_xor(head, 4, 64));
+          if (lane % 8 == 0) heads[0][wave * 8 + lane / 8] = head;
+          __syncthreads();
+          f.bound = reached_by(heads[0], k.top);
+        } else {
+          volatile float* own = heads[wave];
+          own[lane] = head;
+          __builtin_amdgcn_wave_barrier();
+          f.bound = reached_by(heads[wave], k.top);
+        }
+        f.tau = rank_key(f.bound, 0xffffffffu);  // below every class of that logit
+      }
+      const int had = f.n;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (__any(!(top_of[u] < f.bound))) {
+          const int64_t c = at + (u * 64 * NW + tid) * N;
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (__any(!(zs[u][i] < f.bound)))
+              append(list, f, zs[u][i], static_cast<uint32_t>(c + i), c + i < c1);
+        }
+      if (f.n > kList) {
+        f.n = had;
+        append_carefully<T, N, U>(list, f, k.top, z, at + tid * N, 64 * NW * N, c1);
+      }
+    }
   }
-  parts[tid] = p;
-  __syncthreads();
-  for (int o = 128; o >= 1; o >>= 1) {
-    if (tid < o) parts[tid] = join(parts[tid], parts[tid + o], c2);
+
+  // the row's maximum, then its sums
+  float m = wave_max(p.m);
+  if (NW > 1) {
+    if (lane == 0) {
+      red[0][wave] = m;
+      counts[wave] = f.n;
+    }
     __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, red[0][w]);
   }
-  p = parts[0];
-  const bool empty = masked_everywhere(p, k.scale);
-  const float ls = log2f(p.s) * kLn2;
+  move_to(p, m, (p.m - m) * c2 - r);
+  p.s = wave_sum(p.s);
+  p.w = wave_sum(p.w);
+  if (NW > 1) {
+    if (lane == 0) {
+      red[1][wave] = p.s;
+      red[2][wave] = p.w;
+    }
+    __syncthreads();
+    p.s = red[1][0];
+    p.w = red[2][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) {
+      p.s += red[1][w];
+      p.w += red[2][w];
+    }
+  }
+  const float log_s = log2_(p.s) * kLn2;
+  const bool masked = masked_everywhere(p, k.scale);
   if (tid == 0) {
-    if (k.lse) k.lse[row] = empty ? -INFINITY : p.m * k.scale + ls;
-    if (k.entropy) k.entropy[row] = empty ? 0.0f : ls - p.w / p.s * kLn2;
-    if (k.logp) {
-      const int32_t t = k.tokens[row];
-      k.logp[row] = t == -1 ? 0.0f
-                    : t < 0 || t >= V ? NAN
-                    : empty ? -INFINITY
-                            : (load_as_f32(z + t) - p.m) * k.scale - ls;
-    }
+    if (PARTS)
+      cut.stats[blockIdx.x] = p;
+    else
+      write_scores(k, row, p, log_s, masked, zt);
   }
-  uint64_t last = ~uint64_t(0);
-  for (int r = 0; r < k.top; ++r) {
-    uint64_t b = 0;
-    for (int64_t c = tid; c < V; c += 256) {
-      const uint64_t key = rank_key(load_as_f32(z + c), static_cast<uint32_t>(c));
-      if (key < last && key > b) b = key;
+  if (!TOP) return;
+
+  // the rank of each kept key among all of them
+  const auto place = [&](uint64_t key, int rank) {
+    if (rank >= k.top) return;
+    if (PARTS)
+      cut.keys[static_cast<int64_t>(blockIdx.x) * k.top + rank] = key;
+    else
+      write_top(k, row, rank, key, p, log_s, masked);
+  };
+  if (NW == 1) {
+    __builtin_amdgcn_wave_barrier();
+    for (int i = lane; i < f.n; i += 64) {
+      const uint64_t key = list[i];
+      int rank = 0;
+      for (int j = 0; j < f.n; ++j) rank += list[j] > key;
+      place(key, rank);
     }
-    best[tid] = b;
-    __syncthreads();
-    for (int o = 128; o >= 1; o >>= 1) {
-      if (tid < o && best[tid + o] > best[tid]) best[tid] = best[tid + o];
-      __syncthreads();
-    }
-    last = best[0];
-    __syncthreads();
-    if (tid == 0) {
-      k.top_ids[row * k.top + r] = static_cast<int32_t>(key_class(last));
-      k.top_logp[row * k.top + r] = empty ? -INFINITY : (key_logit(last) - p.m) * k.scale - ls;
-    }
+  } else {
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) total += counts[w];
+    for (int w = 0; w < NW; ++w)  // the threads in turn over the lists of the waves
+      for (int i = (tid + 64 * NW - 64 * w) % (64 * NW); i < counts[w]; i += 64 * NW) {
+        const uint64_t key = lists[w][i];
+        int rank = 0;
+        for (int o = 0; o < NW; ++o)
+          for (int j = 0; j < counts[o]; ++j) rank += lists[o][j] > key;
+        place(key, rank);
+      }
+    if (PARTS && tid >= total && tid < k.top)
+      cut.keys[static_cast<int64_t>(blockIdx.x) * k.top + tid] = 0;
   }
 }
 
-template <typename T, typename TD>
-__global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(
-    int64_t V, const T* logits, int64_t ld, float scale, const int32_t* __restrict__ tokens,
-    const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ dlogp,
-    const float* __restrict__ dentropy, TD* dlogits, int64_t ld_out) {
+// The parts of a row: their sums joined in order, and the best of their keys. At least
+// `top` keys reach the least of the parts' q-th ones, q parts' share of `top`, so those
+// below are not ranked.
+constexpr int kMaxParts = 64;
+
+template <typename T>
+__global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores k, Cut cut) {
+  __shared__ uint64_t keys[kMaxParts * kTopMax];
+  __shared__ int count;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x;
-  const T* z = logits + row * ld;
-  TD* d = dlogits + row * ld_out;
-  const float l = lse[row];
-  const float ge = dentropy ? dentropy[row] : 0.0f, H = dentropy ? entropy[row] : 0.0f;
+  const float c2 = k.scale * kLog2e;
+  const float zt = tid == 0 ? token_logit<T>(k, row) : 0.0f;
+  Part p{-INFINITY, 0.0f, 0.0f};
+  if (lane < cut.parts) p = cut.stats[row * cut.parts + lane];
+  const float m = wave_max(p.m);
+  move_to(p, m, (p.m - m) * c2);
+  p.s = wave_sum(p.s);
+  p.w = wave_sum(p.w);
+  const float log_s = log2_(p.s) * kLn2;
+  const bool masked = masked_everywhere(p, k.scale);
+  if (tid == 0) write_scores(k, row, p, log_s, masked, zt);
+  if (k.top == 0) return;
+  if (tid == 0) count = 0;
+  const uint64_t* from = cut.keys + row * cut.parts * k.top;
+  const int share = (k.top + cut.parts - 1) / cut.parts;
+  uint64_t least = lane < cut.parts ? from[lane * k.top + share - 1] : ~uint64_t(0);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const uint64_t other = __shfl_xor(least, o, 64);
+    least = other < least ? other : least;
+  }
+  __syncthreads();
+  for (int i = tid; i < cut.parts * k.top; i += 256) {
+    const uint64_t key = from[i];
+    if (key != 0 && key >= least) keys[atomicAdd(&count, 1)] = key;
+  }
+  __syncthreads();
+  const int n = count;
+  for (int i = tid; i < n; i += 256) {
+    const uint64_t key = keys[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += keys[j] > key;
+    if (rank < k.top) write_top(k, row, rank, key, p, log_s, masked);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Gradient: with p = exp(y - lse) one pass over the logits, -p (dlogp + dentropy (log p + H))
+// and dlogp more at the token. NT threads take a stretch of a row.
+// ---------------------------------------------------------------------------
+struct ScoresGrad {
+  int64_t rows, classes;
+  const void* logits; int64_t ld;
+  float scale;
+  const int32_t* tokens;
+  const float *lse, *entropy, *dlogp, *dentropy;
+  void* dlogits; int64_t ld_out;
+  int chunks;  // stretches of a row
+};
+
+template <typename TD, int N> struct __attribute__((packed, aligned(sizeof(TD)))) OutVec {
+  TD v[N];
+};
+
+template <typename T, typename TD, int NT>
+__global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad k) {
+  constexpr int N = Vec<T>::N, U = kUnroll;
+  const int tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t item = NT == 64 ? static_cast<int64_t>(blockIdx.x) * 4 +
+                                      __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6))
+                                : blockIdx.x;
+  const int64_t row = item / k.chunks;
+  if (row >= k.rows) return;
+  const int64_t at = (item - row * k.chunks) * (NT * N * U);
+  const T* z = static_cast<const T*>(k.logits) + row * k.ld;  // may be dlogits: not restrict
+  TD* d = static_cast<TD*>(k.dlogits) + row * k.ld_out;
+  const float lse = k.lse[row];
+  const float ge = k.dentropy != nullptr ? k.dentropy[row] : 0.0f;
+  const float H = k.dentropy != nullptr ? k.entropy[row] : 0.0f;
   float gl = 0.0f;
-  int64_t t = -1;
-  if (dlogp) {
-    t = tokens[row];
-    gl = t == -1 ? 0.0f : t < 0 || t >= V ? NAN : dlogp[row];
+  int64_t token = -1;
+  if (k.dlogp != nullptr) {
+    token = k.tokens[row];
+    gl = token == -1 ? 0.0f : token < 0 || token >= k.classes ? NAN : k.dlogp[row];
   }
-  for (int64_t c = threadIdx.x; c < V; c += 256) {
-    float g = 0.0f;
-    if (l != -INFINITY) {
-      const float lp = load_as_f32(z + c) * scale - l;
-      const float p = __expf(lp);
-      g = gl * ((c == t ? 1.0f : 0.0f) - p);
-      if (dentropy) g -= ge * (p == 0.0f ? 0.0f : p * (lp + H));
+  const bool masked = lse == -INFINITY && gl == gl;
+  // -scale p (gl + ge (log p + H)) = p (a + b max(log p, -1e4)); p is 0 where the maximum acts
+  const float a = masked ? 0.0f : -k.scale * fmaf(ge, H, gl), b = masked ? 0.0f : -k.scale * ge;
+  const float hot = masked ? 0.0f : k.scale * gl;
+  const float ref = masked ? INFINITY : lse;  // every p of a masked row is 0
+
+  const auto gradient = [&](float v) {
+    const float lp = fmaf(v, k.scale, -ref);
+    const float p = exp2_(lp * kLog2e);
+    return p * fmaf(b, fmaxf(lp, -1e4f), a);
+  };
+  Vec<T> v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t c = at + (u * NT + tid) * N;
+    if (c + N <= k.classes) v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(z + c);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t c = at + (u * NT + tid) * N;
+    if (c + N <= k.classes) {
+      float g[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) g[i] = gradient(v[u][i]);
+      const int64_t own = token - c;
+      if (own >= 0 && own < N)
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] += own == i ? hot : 0.0f;
+      OutVec<TD, N> o;
+#pragma unroll
+      for (int i = 0; i < N; ++i) o.v[i] = store_cast<TD>(g[i]);
+      *reinterpret_cast<OutVec<TD, N>*>(d + c) = o;
+    } else {
+      for (int64_t i = c; i < k.classes; ++i)
+        d[i] = store_cast<TD>(gradient(load_as_f32(z + i)) + (i == token ? hot : 0.0f));
     }
-    d[c] = store_cast<TD>(g * scale);
   }
 }
 
-}  // namespace
+// ---------------------------------------------------------------------------
+// Choice of the variant.
+// ---------------------------------------------------------------------------
+constexpr int64_t kWaveRow = 2048;      // classes up to which a wave takes a row
+constexpr int64_t kPartLen = 4096;      // classes of a part at least
+constexpr int64_t kBlocks = 512;        // workgroups that fill the GPU
+constexpr int64_t kTurn = 1 << 22;      // workgroups of a launch (its threads are counted in 32 bits)
 
-size_t token_scores_ws(int64_t, int64_t, int) { return 256; }
+int parts_of(int64_t rows, int64_t classes, int64_t* len) {
+  *len = classes;
+  if (classes <= kWaveRow || rows >= kBlocks / 2) return 1;
+  int64_t S = kBlocks / rows;
+  if (S > classes / kPartLen) S = classes / kPartLen;
+  if (S > kMaxParts) S = kMaxParts;
+  if (S <= 1) return 1;
+  const int64_t L = ((classes + S - 1) / S + 511) / 512 * 512;
+  *len = L;
+  return static_cast<int>((classes + L - 1) / L);
+}
 
-hipError_t launch_token_scores(const TokenScores& c, void*, hipStream_t s) {
-  launch_kernel(c.dtype == F32 ? dlvm_token_scores_kernel<float> : dlvm_token_scores_kernel<bf16_t>,
-                dim3(static_cast<uint32_t>(c.rows)), dim3(256), s, c);
+template <typename T> hipError_t scores(const TokenScores& c, void* ws, hipStream_t s) {
+  Cut cut{1, c.classes, nullptr, nullptr};
+  if (ws != nullptr) cut.parts = parts_of(c.rows, c.classes, &cut.len);
+  if (cut.parts > 1) {
+    cut.keys = static_cast<uint64_t*>(ws);
+    cut.stats = reinterpret_cast<Part*>(cut.keys + c.rows * cut.parts * c.top);
+    launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, kRowWaves, true, true>
+                            : dlvm_token_scores_kernel<T, kRowWaves, false, true>,
+                  dim3(static_cast<uint32_t>(c.rows * cut.parts)), dim3(64 * kRowWaves), s, c, cut);
+    launch_kernel(dlvm_token_scores_join_kernel<T>, dim3(static_cast<uint32_t>(c.rows)), dim3(256), s, c, cut);
+    return hipGetLastError();
+  }
+  for (int64_t r0 = 0; r0 < c.rows; r0 += kTurn) {
+    TokenScores t = c;
+    t.rows = c.rows - r0 < kTurn ? c.rows - r0 : kTurn;
+    t.logits = static_cast<const T*>(c.logits) + r0 * c.ld;
+    if (c.tokens != nullptr) t.tokens += r0;
+    if (c.logp != nullptr) t.logp += r0;
+    if (c.lse != nullptr) t.lse += r0;
+    if (c.entropy != nullptr) t.entropy += r0;
+    if (c.top > 0) {
+      t.top_ids += r0 * c.top;
+      t.top_logp += r0 * c.top;
+    }
+    if (c.classes <= kWaveRow)
+      launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 1, true, false>
+                              : dlvm_token_scores_kernel<T, 1, false, false>,
+                    dim3(static_cast<uint32_t>((t.rows + 3) / 4)), dim3(256), s, t, cut);
+    else
+      launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, kRowWaves, true, false>
+                              : dlvm_token_scores_kernel<T, kRowWaves, false, false>,
+                    dim3(static_cast<uint32_t>(t.rows)), dim3(64 * kRowWaves), s, t, cut);
+  }
   return hipGetLastError();
 }
 
-namespace {
-template <typename T, typename TD>
-hipError_t grad(int64_t rows, int64_t V, const void* logits, int64_t ld, float scale,
-                const int32_t* tokens, const float* lse, const float* entropy, const float* dlogp,
-                const float* dentropy, void* dlogits, int64_t ld_out, hipStream_t s) {
-  launch_kernel(dlvm_token_scores_grad_kernel<T, TD>, dim3(static_cast<uint32_t>(rows)), dim3(256), s,
-                V, static_cast<const T*>(logits), ld, scale, tokens, lse, entropy, dlogp, dentropy,
-                static_cast<TD*>(dlogits), ld_out);
+template <typename T, typename TD> hipError_t grad(ScoresGrad g, hipStream_t s) {
+  const int NT = g.classes <= kWaveRow ? 64 : 256;
+  const int64_t stretch = NT * Vec<T>::N * kUnroll;
+  const int64_t chunks = (g.classes + stretch - 1) / stretch;
+  g.chunks = static_cast<int>(chunks);
+  const int64_t turn = kTurn / chunks;
+  for (int64_t r0 = 0, rows = g.rows; r0 < rows; r0 += turn) {
+    ScoresGrad h = g;
+    h.rows = rows - r0 < turn ? rows - r0 : turn;
+    h.logits = static_cast<const T*>(g.logits) + r0 * g.ld;
+    h.dlogits = static_cast<TD*>(g.dlogits) + r0 * g.ld_out;
+    h.lse = g.lse + r0;
+    h.tokens = g.tokens ? g.tokens + r0 : nullptr;
+    h.entropy = g.entropy ? g.entropy + r0 : nullptr;
+    h.dlogp = g.dlogp ? g.dlogp + r0 : nullptr;
+    h.dentropy = g.dentropy ? g.dentropy + r0 : nullptr;
+    const int64_t items = h.rows * chunks;
+    launch_kernel(NT == 64 ? dlvm_token_scores_grad_kernel<T, TD, 64> : dlvm_token_scores_grad_kernel<T, TD, 256>,
+                  dim3(static_cast<uint32_t>(NT == 64 ? (items + 3) / 4 : items)), dim3(256), s, h);
+  }
   return hipGetLastError();
 }
+
 }  // namespace
+
+size_t token_scores_ws(int64_t rows, int64_t classes, int top) {
+  int64_t len = 0;
+  const int64_t parts = parts_of(rows, classes, &len);
+  return parts == 1 ? 256 : static_cast<size_t>(rows * parts) * (top * 8 + sizeof(Part));
+}
+
+hipError_t launch_token_scores(const TokenScores& c, void* ws, hipStream_t s) {
+  return c.dtype == F32 ? scores<float>(c, ws, s) : scores<bf16_t>(c, ws, s);
+}
 
 hipError_t launch_token_scores_backward(int dtype, int out_dtype, int64_t rows, int64_t classes,
                                         const void* logits, int64_t ld, float scale,
@@ -174,8 +653,10 @@ hipError_t launch_token_scores_backward(int dtype, int out_dtype, int64_t rows, 
                                         const float* entropy, const float* dlogp,
                                         const float* dentropy, void* dlogits, int64_t ld_out,
                                         hipStream_t s) {
-  auto f = dtype == BF16 ? grad<bf16_t, bf16_t> : out_dtype == BF16 ? grad<float, bf16_t> : grad<float, float>;
-  return f(rows, classes, logits, ld, scale, tokens, lse, entropy, dlogp, dentropy, dlogits, ld_out, s);
+  const ScoresGrad g{rows, classes, logits, ld, scale, tokens, lse, entropy, dlogp, dentropy,
+                     dlogits, ld_out, 1};
+  if (dtype == BF16) return grad<bf16_t, bf16_t>(g, s);
+  return out_dtype == BF16 ? grad<float, bf16_t>(g, s) : grad<float, float>(g, s);
 }
 
 }  // namespace dlvm
