@@ -4,18 +4,20 @@
 //
 // The scores are taken in one pass over the logits. Each thread keeps the running
 // maximum m of its logits and the sums s = sum 2^t and w = sum 2^t t, t the distance of
-// scale z log2(e) from that maximum; they are rescaled once for every 16 or 32 logits, when a
-// new maximum is known. The entropy is log s - w / s: all terms of w have one sign, so it
+// scale z log2(e) from that maximum; they are rescaled once for every 16 logits, when a new
+// maximum is known. The entropy is log s - w / s: all terms of w have one sign, so it
 // has no cancellation beyond its own size. Alternatives are collected in the same pass:
 // from the first tile of a row comes a bound that at least `top` logits reach (the
-// top-th largest of 64 maxima of disjoint parts of it), and the few logits that reach it are
-// kept in LDS, in lists of the waves that are cut back to the `top` best when full. So the
+// top-th largest of 64 maxima of disjoint parts of it, taken again after 2, 4, ... tiles), and
+// the few logits that reach it are kept in LDS, in lists of the waves that are cut back to the `top` best when full. So the
 // common logit costs one comparison for eight, and any order of logits is right.
 // A row is a wave's where it is short, else a workgroup's; with a workspace, a call of few
 // rows cuts them into parts, joined by a second launch.
 // bf16 logits are bound by both memory and arithmetic (about ten operations for two
 // bytes, the exponential four of them), float32 ones by memory.
 #include <math.h>
+
+#include <type_traits>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -51,15 +53,18 @@ __device__ __forceinline__ uint32_t key_class(uint64_t key) {
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float log2_(float v) { return __builtin_amdgcn_logf(v); }
 
+// Sum and maximum over the wave, the same bits in every lane: rotations within rows of 16
+// lanes, then the four rows in order.
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v = row16_sum(v);
+  return ((lane_value(v, 0) + lane_value(v, 16)) + lane_value(v, 32)) + lane_value(v, 48);
 }
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+  v = row16_max(v);
+  return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
 }
 __device__ __forceinline__ int bits_below(uint64_t m) {
   return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32),
@@ -112,6 +117,7 @@ struct Wanted {
   uint64_t tau;
   float bound;
   int n;
+  bool strict;  // the list has been cut back: of equal logits only some are wanted
 };
 
 // Cuts the list back to its `top` best, in order.
@@ -140,13 +146,25 @@ __device__ __forceinline__ void cut_back(volatile uint64_t* list, Wanted& f, int
     const uint32_t low = __builtin_amdgcn_readfirstlane(static_cast<int>(last));
     f.tau = static_cast<uint64_t>(high) << 32 | low;
     f.bound = key_logit(f.tau);
+    f.strict = true;
   }
 }
 
-// One logit of each lane at the end of the list, as far as there is room; counted all the same.
+// How many keys of a list are greater.
+__device__ __forceinline__ int greater_of(const uint64_t* list, int n, uint64_t key) {
+  int rank = 0;
+#pragma unroll 8
+  for (int j = 0; j < n; ++j) rank += list[j] > key;
+  return rank;
+}
+
+// One logit of each lane, where it may be wanted, at the end of the list as far as there is
+// room; counted all the same.
 __device__ __forceinline__ void append(volatile uint64_t* list, Wanted& f, float z, uint32_t c, bool valid) {
+  bool wanted = valid && !(z < f.bound);
+  if (__ballot(wanted) == 0) return;
   const uint64_t key = rank_key(z, c);
-  const bool wanted = valid && key > f.tau;
+  if (f.strict) wanted = wanted && key > f.tau;
   const uint64_t take = __ballot(wanted);
   const int at = f.n + bits_below(take);
   if (wanted && at < kList) list[at] = key;
@@ -157,10 +175,10 @@ __device__ __forceinline__ void append(volatile uint64_t* list, Wanted& f, float
 // room made before each: for the tile that would overflow the list. It reads them again.
 template <typename T, int N, int U>
 __device__ __forceinline__ void append_carefully(volatile uint64_t* list, Wanted& f, int top, const T* z,
-                                                 int64_t c0, int64_t stride, int64_t c1) {
+                                                 int c0, int stride, int c1) {
 #pragma unroll 1
   for (int i = 0; i < U * N; ++i) {
-    const int64_t c = c0 + (i / N) * stride + i % N;
+    const int c = c0 + (i / N) * stride + i % N;
     const bool valid = c < c1;
     const float v = valid ? load_as_f32(z + c) : 0.0f;
     if (f.n + 64 > kList) cut_back(list, f, top);
@@ -168,22 +186,34 @@ __device__ __forceinline__ void append_carefully(volatile uint64_t* list, Wanted
   }
 }
 
-// A logit that at least `top` of 64 values reach: the top-th largest of them.
-__device__ __forceinline__ float reached_by(const float* values, int top) {
-  const float v = values[threadIdx.x & 63];
-  int greater = 0;
-  for (int i = 0; i < 64; i += 4) {
-    const float4 o = *reinterpret_cast<const float4*>(values + i);
-    greater += (o.x > v) + (o.y > v) + (o.z > v) + (o.w > v);
+// A logit that at least `top` of the wave's 64 values reach: the top-th largest with its last
+// 16 bits cleared, found bit by bit from counts of the values that reach a number. (One
+// comparison a bit: 64 values ranked against each other cost more than the rest of a tile.)
+__device__ __forceinline__ float reached_by(float v, int top) {
+  const uint32_t mine = static_cast<uint32_t>(rank_key(v, 0) >> 32);
+  uint32_t reached = 0;
+#pragma unroll
+  for (int b = 31; b >= 16; --b) {
+    const uint32_t with = reached | (1u << b);
+    if (__builtin_popcountll(__ballot(mine >= with)) >= top) reached = with;
   }
-  return -wave_max(greater < top ? -v : -INFINITY);
+  constexpr uint32_t lowest = 0x007fffffu;  // of -infinity
+  return key_logit(static_cast<uint64_t>(reached < lowest ? lowest : reached) << 32);
+}
+
+// Maximum over each eight lanes, in all of them.
+__device__ __forceinline__ float max_of_8(float v) {
+  v = fmaxf(v, row_rot<0xB1>(v));    // the other lane of a pair
+  v = fmaxf(v, row_rot<0x4E>(v));    // the other pair of four
+  return fmaxf(v, row_rot<0x141>(v));  // the other four
 }
 
 // ---------------------------------------------------------------------------
 // Scores. NW waves share a row (or a part of one); NW = 1: four rows to a workgroup.
 // ---------------------------------------------------------------------------
 constexpr int kRowWaves = 8;
-constexpr int kUnroll = 4;  // vectors of a thread in flight
+constexpr int kLogits = 16;  // of a thread in a tile (32 of bf16 took registers for waves: 233 against 218 us)
+constexpr int kUnroll = 4;   // vectors of a thread of the gradient in flight
 
 struct Cut {
   int parts;          // of a row (1: whole rows)
@@ -220,10 +250,10 @@ __device__ __forceinline__ float token_logit(const TokenScores& k, int64_t row) 
 
 template <typename T, int NW, bool TOP, bool PARTS>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_kernel(TokenScores k, Cut cut) {
-  constexpr int N = Vec<T>::N, WAVES = NW == 1 ? 4 : NW, U = kUnroll;
+  constexpr int N = Vec<T>::N, WAVES = NW == 1 ? 4 : NW, U = kLogits / N;
   constexpr int tile = 64 * NW * N * U;  // classes
   __shared__ uint64_t lists[TOP ? WAVES : 1][TOP ? kList : 1];
-  __shared__ __align__(16) float heads[TOP ? (NW == 1 ? 4 : 1) : 1][64];
+  __shared__ float heads[TOP && NW > 1 ? 2 : 1][64];
   __shared__ float red[3][WAVES];
   __shared__ int counts[WAVES];
   const int lane = threadIdx.x & 63;
@@ -237,63 +267,73 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
   }
   if (row >= k.rows) return;  // only whole waves of NW = 1, which meet no barrier
   const T* z = static_cast<const T*>(k.logits) + row * k.ld;
-  const int64_t c0 = PARTS ? part * cut.len : 0;
-  const int64_t c1 = PARTS && c0 + cut.len < k.classes ? c0 + cut.len : k.classes;
+  const int classes = static_cast<int>(k.classes);
+  const int c0 = PARTS ? part * static_cast<int>(cut.len) : 0;
+  const int c1 = PARTS && classes - c0 > cut.len ? c0 + static_cast<int>(cut.len) : classes;
   const float c2 = k.scale * kLog2e;
   const float zt = !PARTS && tid == 0 ? token_logit<T>(k, row) : 0.0f;
 
   Part p{-INFINITY, 0.0f, 0.0f};
   float r = 0.0f;
-  Wanted f{0, -INFINITY, 0};
+  Wanted f{0, -INFINITY, 0, false};
   uint64_t* list = TOP ? lists[wave] : nullptr;
 
+  // The vectors of the tile that starts at class `at`, without a branch for each (it would be
+  // waited for before the next is sent): a vector that would reach over the end of the row
+  // is taken N classes before it. first_of(at, u) is the first class of the thread's u-th, and
+  // from twice_of on its elements are classes that no other vector has.
+  constexpr int stride = 64 * NW * N;
+  const bool tiny = c1 - c0 < N;  // not one vector: an element to each of the first threads
+  const int mine = tid * (tiny ? 1 : N);
+  const auto first_of = [&](int at, int u) {
+    const int c = at + u * stride + mine;
+    return tiny || c <= c1 - N ? c : c1 - N;
+  };
+  const auto twice_of = [&](int at, int u) {
+    const int c = at + u * stride + mine;
+    return c >= c1 ? N : tiny || c <= c1 - N ? 0 : c - (c1 - N);
+  };
   Vec<T> v[U];
-  // The vectors of the tile that starts at class `at`; behind the end of the row, elements of
-  // -infinity.
-  const auto load = [&](int64_t at) {
-    if (at + tile <= c1) {
+  const auto load = [&](int at) {
+    if (tiny) {
+      if (c0 + tid < c1)
+        v[0].raw.w[0] = sizeof(T) == 2 ? reinterpret_cast<const uint16_t*>(z)[c0 + tid]
+                                       : reinterpret_cast<const uint32_t*>(z)[c0 + tid];
+    } else if (c1 - at >= tile) {
+      const T* from = z + at + mine;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(z + at + (u * 64 * NW + tid) * N);
+      for (int u = 0; u < U; ++u) v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(from + u * stride);
     } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t c = at + (u * 64 * NW + tid) * N;
-        if (c + N <= c1) {
-          v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(z + c);
-        } else {
-          constexpr int bits = 8 * sizeof(T);
-          constexpr uint32_t low = bits == 16 ? 0xff80u : 0xff800000u;  // -infinity
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[u].raw.w[i] = 0;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            uint32_t b = low;
-            if (c + i < c1) b = bits == 16 ? reinterpret_cast<const uint16_t*>(z)[c + i]
-                                           : reinterpret_cast<const uint32_t*>(z)[c + i];
-            v[u].raw.w[i * bits / 32] |= b << (i * bits % 32);
-          }
-        }
-      }
+      for (int u = 0; u < U; ++u)
+        if (at + u * stride < c1)
+          v[u].raw = *reinterpret_cast<const typename Vec<T>::Raw*>(z + first_of(at, u));
     }
   };
 
-  load(c0);
-  for (int64_t at = c0; at < c1; at += tile) {
+  // One tile, all of whose vectors are there (WHOLE) or not.
+  unsigned done = 0;  // tiles
+  const auto pass = [&](auto all, int at) {
+    constexpr bool whole = decltype(all)::value;
+    ++done;
     float zs[U][N], top_of[U];
     float big = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float b = -INFINITY;
+      top_of[u] = -INFINITY;
+      if (!whole && at + u * stride >= c1) continue;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        zs[u][i] = v[u][i];
-        b = fmaxf(b, zs[u][i]);
+      for (int i = 0; i < N; ++i) zs[u][i] = v[u][i];
+      if (!whole) {
+        const int from = twice_of(at, u), to = tiny ? 1 : N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) zs[u][i] = i >= from && i < to ? zs[u][i] : -INFINITY;
       }
-      top_of[u] = b;
-      big = fmaxf(big, b);
+#pragma unroll
+      for (int i = 0; i < N; ++i) top_of[u] = fmaxf(top_of[u], zs[u][i]);
+      big = fmaxf(big, top_of[u]);
     }
-    if (at + tile < c1) load(at + tile);
+    if (c1 - at > tile) load(at + tile);
 
     // the maximum so far, and the sums moved to it
     const float m = fmaxf(p.m, big);
@@ -305,7 +345,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
     r = r_new;
     if (plain) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        if (!whole && at + u * stride >= c1) break;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const float t = fmaf(zs[u][i], c2, -M);
@@ -313,9 +354,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
           p.s += e;
           p.w = fmaf(e, fmaxf(t, -1e4f), p.w);  // a masked class: 0 times a finite number
         }
+      }
     } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        if (!whole && at + u * stride >= c1) break;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const float t = (zs[u][i] - ref) * c2;
@@ -323,42 +366,43 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
           p.s += e;
           p.w = fmaf(e, fmaxf(t, -1e4f), p.w);
         }
+      }
     }
 
     if (TOP) {
-      if (at == c0) {
-        float head = big;
+      // after 1, 2, 4, ... tiles: what the maxima so far tell (each wave reads one set while
+      // the next is written to the other)
+      if ((done & (done - 1)) == 0) {
+        float head = m;
         if (NW > 1) {  // of eight threads, so that 64 heads cover the workgroup
-          head = fmaxf(head, __shfl_xor(head, 1, 64));
-          head = fmaxf(head, __shfl_xor(head, 2, 64));
-          head = fmaxf(head, __shfl_xor(head, 4, 64));
-          if (lane % 8 == 0) heads[0][wave * 8 + lane / 8] = head;
+          float* set = heads[__builtin_ctz(done) % 2];
+          head = max_of_8(m);
+          if (lane % 8 == 0) set[wave * 8 + lane / 8] = head;
           __syncthreads();
-          f.bound = reached_by(heads[0], k.top);
-        } else {
-          volatile float* own = heads[wave];
-          own[lane] = head;
-          __builtin_amdgcn_wave_barrier();
-          f.bound = reached_by(heads[wave], k.top);
+          head = set[lane];
         }
-        f.tau = rank_key(f.bound, 0xffffffffu);  // below every class of that logit
+        f.bound = fmaxf(f.bound, lane_value(reached_by(head, k.top), 0));
       }
       const int had = f.n;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (__any(!(top_of[u] < f.bound))) {
-          const int64_t c = at + (u * 64 * NW + tid) * N;
+        if ((whole || at + u * stride < c1) && __any(!(top_of[u] < f.bound))) {
+          const int c = whole ? at + u * stride + mine : first_of(at, u);
+          const int from = whole ? 0 : twice_of(at, u), to = whole || !tiny ? N : 1;
 #pragma unroll
           for (int i = 0; i < N; ++i)
-            if (__any(!(zs[u][i] < f.bound)))
-              append(list, f, zs[u][i], static_cast<uint32_t>(c + i), c + i < c1);
+            append(list, f, zs[u][i], static_cast<uint32_t>(c + i), whole || (i >= from && i < to));
         }
-      if (f.n > kList) {
+      if (f.n > kList) {  // never in a tiny row
         f.n = had;
-        append_carefully<T, N, U>(list, f, k.top, z, at + tid * N, 64 * NW * N, c1);
+        append_carefully<T, N, U>(list, f, k.top, z, at + tid * N, stride, c1);
       }
     }
-  }
+  };
+  load(c0);
+  int at = c0;
+  for (; c1 - at >= tile; at += tile) pass(std::true_type{}, at);
+  if (at < c1) pass(std::false_type{}, at);
 
   // the row's maximum, then its sums
   float m = wave_max(p.m);
@@ -399,7 +443,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
   if (!TOP) return;
 
   // the rank of each kept key among all of them
-  const auto place = [&](uint64_t key, int rank) {
+  const auto put = [&](uint64_t key, int rank) {
     if (rank >= k.top) return;
     if (PARTS)
       cut.keys[static_cast<int64_t>(blockIdx.x) * k.top + rank] = key;
@@ -410,9 +454,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
     __builtin_amdgcn_wave_barrier();
     for (int i = lane; i < f.n; i += 64) {
       const uint64_t key = list[i];
-      int rank = 0;
-      for (int j = 0; j < f.n; ++j) rank += list[j] > key;
-      place(key, rank);
+      put(key, greater_of(list, f.n, key));
     }
   } else {
     int total = 0;
@@ -422,9 +464,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
       for (int i = (tid + 64 * NW - 64 * w) % (64 * NW); i < counts[w]; i += 64 * NW) {
         const uint64_t key = lists[w][i];
         int rank = 0;
-        for (int o = 0; o < NW; ++o)
-          for (int j = 0; j < counts[o]; ++j) rank += lists[o][j] > key;
-        place(key, rank);
+        for (int o = 0; o < NW; ++o) rank += greater_of(lists[o], counts[o], key);
+        put(key, rank);
       }
     if (PARTS && tid >= total && tid < k.top)
       cut.keys[static_cast<int64_t>(blockIdx.x) * k.top + tid] = 0;
@@ -472,8 +513,7 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores
   const int n = count;
   for (int i = tid; i < n; i += 256) {
     const uint64_t key = keys[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += keys[j] > key;
+    const int rank = greater_of(keys, n, key);
     if (rank < k.top) write_top(k, row, rank, key, p, log_s, masked);
   }
 }
