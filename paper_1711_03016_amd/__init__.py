@@ -465,45 +465,53 @@ def sgd(dtype, n, params, master, grads, lr, stream=None):
 # ---------------------------------------------------------------------------
 # sequence operators: token embeddings, gated linear recurrence, token scores
 # ---------------------------------------------------------------------------
-_TYPES = None
+_TORCH = None  # (torch, types by name, current stream's address by device)
 
 
-def _types():
-    """torch types of the storage names, of ids and of workspaces."""
-    global _TYPES
-    if _TYPES is None:
+def _torch():
+    """torch, its types of the storage names, of ids and of workspaces, and what gives the
+    address of the current stream (a stream object made for its address costs half of
+    what a launch does)."""
+    global _TORCH
+    if _TORCH is None:
         import torch
-        _TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "i32": torch.int32,
-                  "ws": torch.uint8}
-    return _TYPES
+        types = {"f32": torch.float32, "bf16": torch.bfloat16, "i32": torch.int32,
+                 "ws": torch.uint8}
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        _TORCH = torch, types, raw
+    return _TORCH
 
 
 def _call(fn, stream, tensors, *args):
     """`fn(*args, stream)` on the GPU of `tensors`, ((name, tensor or None or address,
     type name), ...): tensors of another type, on the host or on a second GPU are refused,
     sizes and strides are the caller's, as in C."""
-    types = _types()
+    torch, types, raw = _TORCH or _torch()
     dev = None
     for name, t, ty in tensors:
-        if t is None or isinstance(t, int):
+        if t is None or t.__class__ is int:
             continue
         if t.dtype is not types[ty]:
             raise DlvmError(ERR_INVALID_ARG, f"{name} is {t.dtype}, not {types[ty]}")
         d = t.get_device()
-        if d < 0:
-            raise DlvmError(ERR_INVALID_ARG, f"{name} is not in GPU memory")
-        if dev is None:
+        if d != dev:
+            if d < 0:
+                raise DlvmError(ERR_INVALID_ARG, f"{name} is not in GPU memory")
+            if dev is not None:
+                raise DlvmError(ERR_INVALID_ARG, f"{name} is on GPU {d}, another tensor on {dev}")
             dev = d
-        elif d != dev:
-            raise DlvmError(ERR_INVALID_ARG, f"{name} is on GPU {d}, another tensor on {dev}")
-    import torch
-    if dev is None or dev == torch.cuda.current_device():
-        _check(fn(*args, _stream(stream)))
-        return
-    if stream is not None and not isinstance(stream, int) and stream.device.index != dev:
-        raise DlvmError(ERR_INVALID_ARG, f"the stream is not on GPU {dev}")
-    with torch.cuda.device(dev):
-        _check(fn(*args, _stream(stream)))
+    if dev is None:
+        status = fn(*args, _stream(stream))
+    elif dev == torch.cuda.current_device():
+        status = fn(*args, raw(dev) if stream is None else _stream(stream))
+    else:
+        if stream is not None and stream.__class__ is not int and stream.device.index != dev:
+            raise DlvmError(ERR_INVALID_ARG, f"the stream is not on GPU {dev}")
+        with torch.cuda.device(dev):
+            status = fn(*args, raw(dev) if stream is None else _stream(stream))
+    if status != OK:
+        _check(status)
 
 
 def _ws_args(ws):

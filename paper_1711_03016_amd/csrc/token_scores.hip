@@ -473,20 +473,33 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
 }
 
 // The parts of a row: their sums joined in order, and the best of their keys. At least
-// `top` keys reach the least of the parts' q-th ones, q parts' share of `top`, so those
-// below are not ranked.
+// `top` keys reach the least of the parts' q-th logits, q parts' share of `top`, so those
+// below are not ranked. All loads are sent before the first is waited for.
 constexpr int kMaxParts = 64;
+constexpr int kJoinKeys = kMaxParts * kTopMax / 256;  // of a thread
 
 template <typename T>
 __global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores k, Cut cut) {
-  __shared__ uint64_t keys[kMaxParts * kTopMax];
+  __shared__ uint64_t keys[256 * kJoinKeys];
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x;
   const float c2 = k.scale * kLog2e;
+  const int share = (k.top + cut.parts - 1) / cut.parts, total = cut.parts * k.top;
+  const uint64_t* from = cut.keys + row * total;
+  const int own = lane < cut.parts ? lane : 0;
+  Part p = cut.stats[row * cut.parts + own];
+  uint64_t mine[kJoinKeys] = {};
+  uint32_t least = 0xffffffffu;
+  if (k.top > 0) {
+    least = static_cast<uint32_t>(from[own * k.top + share - 1] >> 32);
+#pragma unroll
+    for (int i = 0; i < kJoinKeys; ++i)
+      if (256 * i < total) mine[i] = from[tid + 256 * i < total ? tid + 256 * i : total - 1];
+  }
   const float zt = tid == 0 ? token_logit<T>(k, row) : 0.0f;
-  Part p{-INFINITY, 0.0f, 0.0f};
-  if (lane < cut.parts) p = cut.stats[row * cut.parts + lane];
+  if (tid == 0) count = 0;
+  if (lane >= cut.parts) p = Part{-INFINITY, 0.0f, 0.0f};
   const float m = wave_max(p.m);
   move_to(p, m, (p.m - m) * c2);
   p.s = wave_sum(p.s);
@@ -495,20 +508,16 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores
   const bool masked = masked_everywhere(p, k.scale);
   if (tid == 0) write_scores(k, row, p, log_s, masked, zt);
   if (k.top == 0) return;
-  if (tid == 0) count = 0;
-  const uint64_t* from = cut.keys + row * cut.parts * k.top;
-  const int share = (k.top + cut.parts - 1) / cut.parts;
-  uint64_t least = lane < cut.parts ? from[lane * k.top + share - 1] : ~uint64_t(0);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
-    const uint64_t other = __shfl_xor(least, o, 64);
+    const uint32_t other = __shfl_xor(least, o, 64);
     least = other < least ? other : least;
   }
   __syncthreads();
-  for (int i = tid; i < cut.parts * k.top; i += 256) {
-    const uint64_t key = from[i];
-    if (key != 0 && key >= least) keys[atomicAdd(&count, 1)] = key;
-  }
+#pragma unroll
+  for (int i = 0; i < kJoinKeys; ++i)
+    if (tid + 256 * i < total && mine[i] != 0 && static_cast<uint32_t>(mine[i] >> 32) >= least)
+      keys[atomicAdd(&count, 1)] = mine[i];
   __syncthreads();
   const int n = count;
   for (int i = tid; i < n; i += 256) {
