@@ -1,11 +1,11 @@
 // Token embeddings: the lookup with scaling, and the gradient of the table by
 // sorted tokens.
 //
-// The gradient, dtable[v] = scale * sum of dout[i] over the tokens i with id v, runs in
-// three launches and no floating-point atomics: tokens are grouped by id in their
-// order (and the rows without a token are zeroed by the same launch, which is most of
-// the bytes of a large table), equal pieces of the grouped list are summed, and the
-// sums of rows that run over a piece's end are joined in the order of the pieces.
+// The gradient, dtable[v] = scale * sum of dout[i] over the tokens i with id v, uses no
+// floating-point atomics: the tokens are sorted by id, equal pieces of the sorted list are
+// summed (by the launch that zeroes the rows without a token, most of the bytes of a large
+// table), and the sums of rows that run over a piece's end are joined in the order of the
+// pieces.
 #include <math.h>
 
 #include "common.hpp"
@@ -84,28 +84,27 @@ __global__ __launch_bounds__(256) void dlvm_embedding_kernel(uint32_t V, int64_t
 }
 
 // ---------------------------------------------------------------------------
-// Gradient, launch 1: tokens grouped by id. Every workgroup reads all ids (a few
-// hundred KB, from the L2) and takes those whose low bits are its number, so frequent
-// ids, which are neighbours in most vocabularies, fall to different workgroups. The
-// ids of lower-numbered groups, counted on the way, are where its list starts: no
-// launch has to scan counts. Each of its waves owns a contiguous range of tokens, a row
-// of counters and a list in LDS of the tokens it took, so that they are placed in one
-// order (ranges ascending; within 256 tokens every fourth one, from each of the first
-// four) without any order between waves; a wave whose list is full (one id
-// is a tenth of many tokens) reads its range again instead. What a vector of 64 ids
-// costs in the reading is what bounds it, 256 times over: three comparisons with scalar
-// counts of their masks, and a branch. The rows that have
-// no token are zeroed before the tokens are placed.
+// Gradient, the sort: stable, by digits of kDigitBits from the lowest, two launches to a
+// digit: blocks of tokens count their digits, and place them from the counts of all
+// blocks. Counts are whole numbers, so nothing depends on an order of execution, and a
+// frequent id costs no more than others. Each wave of a block owns consecutive
+// tokens; the lanes of one digit find each other by a ballot to each of its bits. Up to
+// kSmallSort tokens are sorted by one workgroup in LDS. Ids outside the table are taken as
+// V, one more than the last row: they come last and are left out of the sums. (Choosing a
+// row's tokens from all ids, one workgroup to some rows and without a sort, took 52 us for
+// 200001 tokens of 1021 rows, for the sake of the most frequent row alone.)
 // ---------------------------------------------------------------------------
-constexpr int kSortThreads = 1024;
+constexpr int kDigitBits = 10;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kSortThreads = kDigits;                // one thread to a digit
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortRows = 512;                       // rows of one group at most
-constexpr int kSortMinGroups = 256;                  // a workgroup on every compute unit
-constexpr int64_t kSortTokens = int64_t(1) << 18;    // tokens of one sorting launch
-constexpr int kSortUnroll = 8;
-constexpr int kSortList = 1536;                      // tokens of a wave's list
-constexpr int kSortRowBits = 9;                      // 2^9 = kSortRows; the rest: token in the wave's range
-static_assert((1 << kSortRowBits) == kSortRows && kSortTokens / kSortWaves <= (1 << (32 - kSortRowBits)), "");
+constexpr int kSortBlock = 4 * kSortThreads;         // tokens of a block
+constexpr int kSmallSort = 8 * kSortThreads;
+constexpr int64_t kSortTokens = int64_t(1) << 18;    // tokens of one sort
+
+__device__ __forceinline__ int32_t row_of(int32_t id, int32_t V) {
+  return static_cast<uint32_t>(id) < static_cast<uint32_t>(V) ? id : V;
+}
 
 // Set bits below the lane's.
 __device__ __forceinline__ int bits_below(uint64_t m) {
@@ -113,180 +112,220 @@ __device__ __forceinline__ int bits_below(uint64_t m) {
                                    __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
 }
 
-// Places of the tokens of one vector in a wave's part of the grouped list: `row` of the
-// lane's token (-1: none), one row of the vector at a time; `next` the wave's counters, of
-// which that of the row last placed is kept in `hot` and `at_hot` (a frequent id is
-// placed vector after vector without waiting for LDS).
-__device__ __forceinline__ void place_tokens(int row, int32_t tok, int32_t id, volatile int32_t* next,
-                                             int& hot, int32_t& at_hot, int32_t* __restrict__ stok,
-                                             int32_t* __restrict__ sid) {
-  uint64_t todo = __ballot(row >= 0);
-  while (todo != 0) {
-    const int one = __builtin_amdgcn_readlane(row, __builtin_ctzll(todo));
-    const uint64_t same = __ballot(row == one);
-    if (one != hot) {
-      if (hot >= 0) next[hot] = at_hot;
-      hot = one;
-      at_hot = __builtin_amdgcn_readfirstlane(next[one]);
+// Ranks of W vectors of 64 digits of `bits` bits (lanes `on`) among the equal ones of the wave so
+// far, whose counts are kept in `counts`.
+template <int W>
+__device__ __forceinline__ void rank_digits(const int32_t (&digit)[W], const bool (&on)[W], int bits,
+                                            int32_t (&rank)[W], volatile int32_t* counts) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    uint64_t same = __ballot(on[i]);
+    if (same == 0) break;  // the vectors behind the last token
+    for (int b = 0; b < bits; ++b) {
+      const bool bit = (digit[i] >> b) & 1;
+      const uint64_t set = __ballot(bit);
+      same &= bit ? set : ~set;
     }
-    if (row == one) {
-      const int32_t at = at_hot + bits_below(same);
-      stok[at] = tok;
-      sid[at] = id;
+    const int before = bits_below(same);
+    if (on[i]) {
+      const int32_t so_far = counts[digit[i]];
+      rank[i] = so_far + before;
+      if (before == 0) counts[digit[i]] = so_far + __builtin_popcountll(same);
     }
-    at_hot += __builtin_popcountll(same);
-    todo &= ~same;
   }
 }
 
-// Four consecutive ids of a lane from token i on, -1 behind `end` (ids start on 16 bytes,
-// i is a multiple of 4).
-__device__ __forceinline__ int4 load_ids(const int32_t* __restrict__ ids, int32_t i, int32_t end) {
-  int4 v = make_int4(-1, -1, -1, -1);
-  if (i + 4 <= end) {
-    v = *reinterpret_cast<const int4*>(ids + i);
-  } else if (i < end) {
-    v.x = ids[i];
-    if (i + 1 < end) v.y = ids[i + 1];
-    if (i + 2 < end) v.z = ids[i + 2];
+// Exclusive sum of one number of each of kSortThreads threads.
+__device__ __forceinline__ int32_t exclusive_sum(int32_t v, int32_t* sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int32_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t up = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += up;
   }
-  return v;
+  if (lane == 63) sums[wave] = incl;
+  __syncthreads();
+  int32_t at = incl - v;
+  for (int w = 0; w < wave; ++w) at += sums[w];
+  return at;
 }
 
-template <bool ZERO>
-__global__ __launch_bounds__(kSortThreads) void dlvm_embedding_group_kernel(
-    uint32_t V, int64_t E, int32_t N, int log_groups, const int32_t* __restrict__ ids,
-    int32_t* __restrict__ count, int32_t* __restrict__ stok, int32_t* __restrict__ sid,
-    float* __restrict__ dtable) {
-  __shared__ int32_t hist[kSortWaves][kSortRows];
-  __shared__ uint32_t list[kSortWaves][kSortList];
-  __shared__ int32_t lower[kSortWaves];
-  __shared__ int32_t sums[kSortRows / 64];
-  __shared__ uint8_t used[kSortRows];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t me = blockIdx.x, mask = (1u << log_groups) - 1;
-  const int R = static_cast<int>((V + mask) >> log_groups);
-  for (int w = 0; w < kSortWaves; ++w)
-    if (tid < R) hist[w][tid] = 0;
-  __syncthreads();
+// The waves' counts of the thread's digit, and their sum.
+__device__ __forceinline__ int32_t take_counts(const int32_t (*counts)[kDigits], int32_t (&n)[kSortWaves]) {
+  int32_t all = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    n[w] = counts[w][threadIdx.x];
+    all += n[w];
+  }
+  return all;
+}
+// Turns them into places: `base` is where the digit begins.
+__device__ __forceinline__ void place_waves(int32_t (*counts)[kDigits], const int32_t (&n)[kSortWaves],
+                                            int32_t base) {
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    counts[w][threadIdx.x] = base;
+    base += n[w];
+  }
+}
 
-  const int32_t span = (N + 4 * kSortThreads - 1) / (4 * kSortThreads) * 256;  // tokens of a wave
-  const int32_t first = wave * span;
-  const int32_t end = first + span < N ? first + span : N;
-  int32_t below = 0, taken = 0;  // of this wave
-  for (int32_t i0 = first; i0 < end; i0 += 256 * kSortUnroll) {
-    int4 id[kSortUnroll];
+// Where the tokens of a pass come from: ids (first pass) or pairs sorted by lower digits.
+struct SortIn {
+  const int32_t* ids;
+  const int32_t* row;
+  const int32_t* tok;
+};
+
+__global__ __launch_bounds__(kSortThreads) void dlvm_embedding_count_kernel(int32_t V, int32_t N, int shift,
+                                                                            int bits, SortIn in,
+                                                                            int32_t* __restrict__ counts) {
+  __shared__ int32_t hist[kDigits];
+  hist[threadIdx.x] = 0;
+  __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kSortUnroll; ++u) id[u] = load_ids(ids, i0 + 256 * u + 4 * lane, end);
+  for (int u = 0; u < kSortBlock / kSortThreads; ++u) {
+    const int32_t i = blockIdx.x * kSortBlock + u * kSortThreads + threadIdx.x;
+    if (i < N) {
+      const int32_t row = in.ids != nullptr ? row_of(in.ids[i], V) : in.row[i];
+      atomicAdd(&hist[(row >> shift) & ((1 << bits) - 1)], 1);
+    }
+  }
+  __syncthreads();
+  counts[blockIdx.x * kDigits + threadIdx.x] = hist[threadIdx.x];
+}
+
+__global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
+    int32_t V, int32_t N, int shift, int bits, SortIn in, const int32_t* __restrict__ counts,
+    int32_t* __restrict__ row_out, int32_t* __restrict__ tok_out) {
+  constexpr int W = kSortBlock / kSortThreads;
+  __shared__ int32_t places[kSortWaves][kDigits];
+  __shared__ int32_t sums[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
-    for (int u = 0; u < kSortUnroll; ++u) {
-      const uint32_t v[4] = {static_cast<uint32_t>(id[u].x), static_cast<uint32_t>(id[u].y),
-                             static_cast<uint32_t>(id[u].z), static_cast<uint32_t>(id[u].w)};
-      bool hit[4];
+  for (int w = 0; w < kSortWaves; ++w) places[w][tid] = 0;
+  int32_t row[W], tok[W], digit[W], rank[W];
+  bool on[W];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool valid = v[j] < V;
-        hit[j] = valid && (v[j] & mask) == me;
-        below += __builtin_popcountll(__ballot(valid && (v[j] & mask) < me));
+  for (int u = 0; u < W; ++u) {
+    const int32_t i = blockIdx.x * kSortBlock + wave * 64 * W + u * 64 + lane;
+    on[u] = i < N;
+    const int32_t at = on[u] ? i : N - 1;
+    row[u] = in.ids != nullptr ? row_of(in.ids[at], V) : in.row[at];
+    tok[u] = in.ids != nullptr ? at : in.tok[at];
+    digit[u] = (row[u] >> shift) & ((1 << bits) - 1);
+  }
+  // of the thread's digit: tokens of earlier blocks, and of all
+  int32_t earlier = 0, all = 0;
+#pragma unroll 16
+  for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
+    const int32_t n = counts[b * kDigits + tid];
+    all += n;
+    if (b < static_cast<int>(blockIdx.x)) earlier += n;
+  }
+  const int32_t first = exclusive_sum(all, sums);  // its barrier also follows the zeros above
+  rank_digits<W>(digit, on, bits, rank, places[wave]);
+  __syncthreads();
+  int32_t n[kSortWaves];
+  take_counts(places, n);
+  place_waves(places, n, first + earlier);
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < W; ++u)
+    if (on[u]) {
+      const int32_t at = places[wave][digit[u]] + rank[u];
+      row_out[at] = row[u];
+      tok_out[at] = tok[u];
+    }
+}
+
+__global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(int32_t V, int32_t N, int bits, int digit_bits,
+                                                                           const int32_t* __restrict__ ids,
+                                                                           int32_t* __restrict__ row_out,
+                                                                           int32_t* __restrict__ tok_out) {
+  constexpr int W = kSmallSort / kSortThreads;
+  __shared__ int32_t places[kSortWaves][kDigits];
+  __shared__ int32_t rows[kSmallSort];
+  __shared__ uint16_t toks[kSmallSort];
+  __shared__ int32_t sums[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int span = (N + kSortThreads - 1) / kSortThreads * 64;  // tokens of a wave
+  const int first = wave * span + lane;
+  int32_t row[W], tok[W], digit[W], rank[W];
+  bool on[W];
+#pragma unroll
+  for (int u = 0; u < W; ++u) {
+    const int32_t i = first + u * 64;
+    on[u] = u * 64 < span && i < N;
+    row[u] = row_of(ids[on[u] ? i : N - 1], V);
+    tok[u] = i;
+  }
+  for (int shift = 0;; shift += digit_bits) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) places[w][tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < W; ++u) digit[u] = (row[u] >> shift) & ((1 << digit_bits) - 1);
+    rank_digits<W>(digit, on, digit_bits, rank, places[wave]);
+    __syncthreads();
+    int32_t n[kSortWaves];
+    const int32_t all = take_counts(places, n);
+    place_waves(places, n, exclusive_sum(all, sums));
+    __syncthreads();
+    const bool last = shift + digit_bits >= bits;
+#pragma unroll
+    for (int u = 0; u < W; ++u)
+      if (on[u]) {
+        const int32_t at = places[wave][digit[u]] + rank[u];
+        if (last) {
+          row_out[at] = row[u];
+          tok_out[at] = tok[u];
+        } else {
+          rows[at] = row[u];
+          toks[at] = static_cast<uint16_t>(tok[u]);
+        }
       }
+    if (last) return;
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t match = __ballot(hit[j]);
-        if (match == 0) continue;
-        const int32_t at = taken + bits_below(match);
-        if (hit[j] && at < kSortList)
-          list[wave][at] = static_cast<uint32_t>(i0 - first + 256 * u + 4 * lane + j) << kSortRowBits |
-                           v[j] >> log_groups;
-        taken += __builtin_popcountll(match);
+    for (int u = 0; u < W; ++u)
+      if (on[u]) {
+        row[u] = rows[first + u * 64];
+        tok[u] = toks[first + u * 64];
       }
-    }
-  }
-  if (lane == 0) lower[wave] = below;
-  if (taken <= kSortList) {
-    for (int j = lane; j < taken; j += 64) atomicAdd(&hist[wave][list[wave][j] & (kSortRows - 1)], 1);
-  } else {
-    for (int32_t i = first + lane; i < end; i += 64) {
-      const uint32_t v = static_cast<uint32_t>(ids[i]);
-      if (v < V && (v & mask) == me) atomicAdd(&hist[wave][v >> log_groups], 1);
-    }
-  }
-  __syncthreads();
-
-  // counts to places: exclusive sums over the rows, and within a row over the waves
-  int32_t mine = 0, incl = 0;
-  if (tid < kSortRows) {
-    if (tid < R)
-      for (int w = 0; w < kSortWaves; ++w) mine += hist[w][tid];
-    used[tid] = mine != 0;
-    incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int32_t up = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += up;
-    }
-    if (lane == 63) sums[wave] = incl;
-  }
-  __syncthreads();
-  if (tid < kSortRows) {
-    int32_t at = incl - mine;
-    for (int w = 0; w < kSortWaves; ++w) at += lower[w];
-    for (int w = 0; w < wave; ++w) at += sums[w];
-    if (tid == kSortRows - 1 && me == mask) *count = at + mine;
-    if (tid < R)
-      for (int w = 0; w < kSortWaves; ++w) {
-        const int32_t n = hist[w][tid];
-        hist[w][tid] = at;
-        at += n;
-      }
-  }
-  __syncthreads();
-
-  if (ZERO) {
-    using Vec = Elems<float, 4>;
-    const Vec zero{{0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int r = wave; r < R; r += kSortWaves) {
-      const uint32_t v = (static_cast<uint32_t>(r) << log_groups) + me;
-      if (used[r] || v >= V) continue;
-      float* row = dtable + v * E;
-      int64_t c = 4 * lane;
-      for (; c + 4 <= E; c += 256) *reinterpret_cast<Vec*>(row + c) = zero;
-      for (; c < E; ++c) row[c] = 0.0f;
-    }
-  }
-
-  volatile int32_t* next = hist[wave];
-  int hot = -1;
-  int32_t at_hot = 0;
-  if (taken <= kSortList) {
-    for (int j = 0; j < taken; j += 64) {
-      const uint32_t e = j + lane < taken ? list[wave][j + lane] : 0;
-      const int row = j + lane < taken ? static_cast<int>(e & (kSortRows - 1)) : -1;
-      place_tokens(row, first + static_cast<int32_t>(e >> kSortRowBits),
-                   static_cast<int32_t>((e & (kSortRows - 1)) << log_groups | me), next, hot, at_hot,
-                   stok, sid);
-    }
-    return;
-  }
-  for (int32_t i0 = first; i0 < end; i0 += 256) {
-    const int4 id = load_ids(ids, i0 + 4 * lane, end);
-    const int32_t v[4] = {id.x, id.y, id.z, id.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t u = static_cast<uint32_t>(v[j]);
-      const int row = u < V && (u & mask) == me ? static_cast<int>(u >> log_groups) : -1;
-      place_tokens(row, i0 + 4 * lane + j, v[j], next, hot, at_hot, stok, sid);
-    }
   }
 }
 
 // ---------------------------------------------------------------------------
-// Gradient, launch 2: a wave sums one piece of the grouped list over a slab of
+// Gradient, the sums: a wave sums one piece of the sorted list over a slab of
 // 64 * VEC * G columns (G vectors a lane, each contiguous over the wave), eight rows in
 // flight. Rows that begin and end inside a piece are written; what belongs to a row that
 // began in an earlier piece goes to `head`, the start of one that goes on in the next
-// piece to `tail` (float32, without the scale).
+// piece to `tail` (float32, without the scale). The workgroups behind those of the pieces zero
+// the rows that have no token, 64 to a wave, each found absent by a search of the list.
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ void zero_absent(int32_t V, int64_t E, int32_t N, int64_t first,
+                                            const int32_t* __restrict__ sid, float* __restrict__ dtable) {
+  using Quad = Elems<float, 4>;
+  const int lane = threadIdx.x & 63;
+  const int64_t v = first + lane;
+  int32_t lo = 0, hi = N;  // the first place that holds v or more
+  while (lo < hi) {
+    const int32_t mid = (lo + hi) >> 1;
+    if (sid[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  const bool absent = v < V && !(lo < N && sid[lo] == v);
+  const Quad zero{{0.0f, 0.0f, 0.0f, 0.0f}};
+  for (uint64_t todo = __ballot(absent); todo != 0; todo &= todo - 1) {
+    float* row = dtable + (first + __builtin_ctzll(todo)) * E;
+    int64_t c = 4 * lane;
+    for (; c + 4 <= E; c += 256) *reinterpret_cast<Quad*>(row + c) = zero;
+    for (; c < E; ++c) row[c] = 0.0f;
+  }
+}
+
 template <int VEC, int G>
 __device__ __forceinline__ void store_row(float* __restrict__ to, const int64_t (&c)[G], const bool (&on)[G],
                                           bool add, float scale, float (&acc)[G][VEC]) {
@@ -311,19 +350,22 @@ __device__ __forceinline__ void store_row(float* __restrict__ to, const int64_t 
 
 template <typename T, int VEC, int G>
 __global__ __launch_bounds__(256) void dlvm_embedding_pieces_kernel(
-    int64_t E, int P, int pieces, int slabs, const int32_t* __restrict__ count,
+    int32_t V, int64_t E, int P, int pieces, int slabs, int sum_blocks, int32_t total,
     const int32_t* __restrict__ stok, const int32_t* __restrict__ sid, const T* __restrict__ dout,
     float scale, bool accumulate, float* __restrict__ head, float* __restrict__ tail,
     float* __restrict__ dtable) {
   using Vec = Elems<T, VEC>;
   constexpr int kUnroll = 8;
   const int lane = threadIdx.x & 63;
-  const int task = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+  if (static_cast<int>(blockIdx.x) >= sum_blocks) {
+    zero_absent(V, E, total, (static_cast<int64_t>(blockIdx.x - sum_blocks) * 4 + wave) * 64, sid, dtable);
+    return;
+  }
+  const int task = static_cast<int>(blockIdx.x) * 4 + wave;
   const int piece = task / slabs;
   if (piece >= pieces) return;
-  const int32_t total = *count;
   const int32_t p0 = piece * P;
-  if (p0 >= total) return;
   const int n = total - p0 < P ? total - p0 : P;
   const int32_t tok = lane < n ? stok[p0 + lane] : 0;
   const int32_t id = lane < n ? sid[p0 + lane] : -1;
@@ -360,7 +402,7 @@ __global__ __launch_bounds__(256) void dlvm_embedding_pieces_kernel(
       const bool live = i0 + u < n;
       const int32_t next = live ? __builtin_amdgcn_readlane(id, i0 + u) : cur;
       if (next != cur) {
-        if (begins)
+        if (begins)  // rows come in order: not V, after which there is none
           store_row<VEC, G>(dtable + cur * E, c, on, accumulate, scale, acc);
         else
           store_row<VEC, G>(head + part, c, on, false, 1.0f, acc);
@@ -374,6 +416,7 @@ __global__ __launch_bounds__(256) void dlvm_embedding_pieces_kernel(
           for (int k = 0; k < VEC; ++k) acc[g][k] += load_as_f32(&w[u][g].v[k]);
     }
   }
+  if (cur == V) return;
   if (begins && cur != after)
     store_row<VEC, G>(dtable + cur * E, c, on, accumulate, scale, acc);
   else
@@ -381,7 +424,7 @@ __global__ __launch_bounds__(256) void dlvm_embedding_pieces_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// Gradient, launch 3: the rows that run over the end of the piece they begin in: the
+// Gradient, the joins: the rows that run over the end of the piece they begin in: the
 // piece's tail and the heads of the following pieces up to the row's last, added in
 // order. Rows of few parts take one wave to 256 columns; rows that fill at least
 // kJoinLong whole pieces a workgroup, whose waves take equal ranges of the parts and
@@ -435,20 +478,19 @@ __device__ __forceinline__ void add_parts(int64_t E, int64_t p, int from, int to
 }
 
 __global__ __launch_bounds__(64 * kJoinWaves) void dlvm_embedding_join_kernel(
-    int64_t E, int P, int pieces, int slabs, int short_blocks, const int32_t* __restrict__ count,
+    int32_t V, int64_t E, int P, int pieces, int slabs, int short_blocks, int32_t total,
     const int32_t* __restrict__ sid, float scale, bool accumulate, const float* __restrict__ head,
     const float* __restrict__ tail, float* __restrict__ dtable) {
   __shared__ float part[kJoinWaves][kJoinCols];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  const int32_t total = *count;
 
   if (static_cast<int>(blockIdx.x) < short_blocks) {
     const int task = blockIdx.x * kJoinWaves + wave;
     const int p = task / slabs;
     if (p >= pieces || static_cast<int64_t>(p + 1) * P >= total) return;
     const int32_t id = sid[(p + 1) * P - 1];
-    if (!crosses(sid, total, P, p, id) || came_in(sid, P, p)) return;
+    if (id == V || !crosses(sid, total, P, p, id) || came_in(sid, P, p)) return;
     // parts after the first: pieces p + 1 .. p + more, the last the one whose end it does not cross
     const bool on = lane <= kJoinLong && crosses(sid, total, P, p + 1 + lane, id);
     const int more = __builtin_ctzll(~__ballot(on)) + 1;
@@ -467,7 +509,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void dlvm_embedding_join_kernel(
   const int64_t q = static_cast<int64_t>(task / slabs + 1) * kJoinLong - 1;
   if (q >= pieces || (q + 1) * P >= total) return;
   const int32_t id = sid[(q + 1) * P - 1];
-  if (!crosses(sid, total, P, q, id)) return;
+  if (id == V || !crosses(sid, total, P, q, id)) return;
   // where the row begins: here or in one of the kJoinLong - 1 pieces before
   const bool in = lane < kJoinLong && came_in(sid, P, q - lane);
   const int back = __builtin_ctzll(~__ballot(in));
@@ -508,8 +550,9 @@ int piece_len(int64_t width, int64_t tokens) {
   return waves >= 64 * 2048 ? 64 : waves >= 32 * 2048 ? 32 : 16;
 }
 
+// Workspace of a gradient call: pairs (row, token) before and after a pass, counts, partial sums.
 struct GradWs {
-  size_t count, stok, sid, head, tail, total;
+  size_t row[2], tok[2], counts, head, tail, total;
   int P;
   int64_t chunk, pieces;
 };
@@ -519,13 +562,40 @@ GradWs grad_ws(int64_t width, int64_t tokens) {
   w.chunk = tokens < kSortTokens ? tokens : kSortTokens;
   w.P = piece_len(width, w.chunk);
   w.pieces = (w.chunk + w.P - 1) / w.P;
-  w.count = 0;
-  w.stok = 256;
-  w.sid = w.stok + up(static_cast<size_t>(w.chunk) * 4);
-  w.head = w.sid + up(static_cast<size_t>(w.chunk) * 4);
+  const size_t list = up(static_cast<size_t>(w.chunk) * 4);
+  for (int i = 0; i < 2; ++i) {
+    w.row[i] = 2 * i * list;
+    w.tok[i] = (2 * i + 1) * list;
+  }
+  w.counts = 4 * list;
+  w.head = w.counts + static_cast<size_t>((w.chunk + kSortBlock - 1) / kSortBlock) * kDigits * 4;
   w.tail = w.head + up(static_cast<size_t>(w.pieces) * width * 4);
   w.total = w.tail + up(static_cast<size_t>(w.pieces) * width * 4);
   return w;
+}
+
+// The call's n tokens sorted by row; returns which of the two lists holds them.
+int sort_tokens(const GradWs& w, int32_t V, int32_t n, const int32_t* ids, char* ws, hipStream_t s) {
+  const auto list = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
+  int bits = 1;  // of the largest key, V
+  while ((V >> bits) != 0) ++bits;
+  const int passes = (bits + kDigitBits - 1) / kDigitBits, digit_bits = (bits + passes - 1) / passes;
+  if (n <= kSmallSort) {
+    launch_kernel(dlvm_embedding_sort_kernel, dim3(1), dim3(kSortThreads), s, V, n, bits, digit_bits, ids,
+                  list(w.row[0]), list(w.tok[0]));
+    return 0;
+  }
+  const dim3 blocks(static_cast<uint32_t>((n + kSortBlock - 1) / kSortBlock));
+  int to = 0;
+  for (int shift = 0; shift < bits; shift += digit_bits, to ^= 1) {
+    const SortIn in = shift == 0 ? SortIn{ids, nullptr, nullptr}
+                                 : SortIn{nullptr, list(w.row[to ^ 1]), list(w.tok[to ^ 1])};
+    launch_kernel(dlvm_embedding_count_kernel, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits,
+                  in, list(w.counts));
+    launch_kernel(dlvm_embedding_place_kernel, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits, in,
+                  static_cast<const int32_t*>(list(w.counts)), list(w.row[to]), list(w.tok[to]));
+  }
+  return to ^ 1;
 }
 
 template <typename T, int VEC>
@@ -545,27 +615,36 @@ void lookup(int64_t V, int64_t E, int64_t N, const void* table, const int32_t* i
   }
 }
 
+// One chunk of tokens, sorted.
+struct Chunk {
+  int32_t V;
+  int64_t E;
+  int32_t n;
+  const int32_t *row, *tok;
+  float scale;
+  bool add;
+  float *head, *tail, *dtable;
+  int P;
+};
+
 template <typename T, int VEC, int G>
-void sum_pieces(const GradWs& w, int64_t E, int64_t n, char* ws, const T* dout, float scale,
-                bool accumulate, float* dtable, hipStream_t s) {
-  const int64_t pieces = (n + w.P - 1) / w.P, slabs = (E + 64 * VEC * G - 1) / (64 * VEC * G);
-  launch_kernel(dlvm_embedding_pieces_kernel<T, VEC, G>, dim3(static_cast<uint32_t>((pieces * slabs + 3) / 4)),
-                dim3(256), s, E, w.P, static_cast<int>(pieces), static_cast<int>(slabs),
-                reinterpret_cast<const int32_t*>(ws + w.count), reinterpret_cast<const int32_t*>(ws + w.stok),
-                reinterpret_cast<const int32_t*>(ws + w.sid), dout, scale, accumulate,
-                reinterpret_cast<float*>(ws + w.head), reinterpret_cast<float*>(ws + w.tail), dtable);
+void sum_pieces(const Chunk& c, const T* dout, hipStream_t s) {
+  const int64_t pieces = (c.n + c.P - 1) / c.P, slabs = (c.E + 64 * VEC * G - 1) / (64 * VEC * G);
+  const int64_t sum_blocks = (pieces * slabs + 3) / 4, zero_blocks = c.add ? 0 : (c.V + 255) / 256;
+  launch_kernel(dlvm_embedding_pieces_kernel<T, VEC, G>, dim3(static_cast<uint32_t>(sum_blocks + zero_blocks)),
+                dim3(256), s, c.V, c.E, c.P, static_cast<int>(pieces), static_cast<int>(slabs),
+                static_cast<int>(sum_blocks), c.n, c.tok, c.row, dout, c.scale, c.add, c.head, c.tail, c.dtable);
 }
 
 // The widest vector that divides the row, and as many to a lane as leave none idle.
-template <typename T>
-void sum_pieces_any(const GradWs& w, int64_t E, int64_t n, char* ws, const T* dout, float scale,
-                    bool accumulate, float* dtable, hipStream_t s) {
+template <typename T> void sum_pieces_any(const Chunk& c, const T* dout, hipStream_t s) {
+  const int64_t E = c.E;
   auto f = E % 4 == 0 && E >= 512 ? sum_pieces<T, 4, 2>
            : E % 4 == 0 && E >= 256 ? sum_pieces<T, 4, 1>
            : E % 2 == 0 && E >= 256 ? sum_pieces<T, 2, 2>
            : E % 2 == 0 && E >= 128 ? sum_pieces<T, 2, 1>
            : E >= 256 ? sum_pieces<T, 1, 4> : sum_pieces<T, 1, 1>;
-  f(w, E, n, ws, dout, scale, accumulate, dtable, s);
+  f(c, dout, s);
 }
 
 }  // namespace
@@ -589,31 +668,24 @@ hipError_t launch_embedding_backward(int dtype, int64_t vocab, int64_t width, in
                                      bool accumulate, float* dtable, void* ws, hipStream_t s) {
   const GradWs w = grad_ws(width, tokens);
   char* base = static_cast<char*>(ws);
-  int32_t* count = reinterpret_cast<int32_t*>(base + w.count);
-  int32_t* stok = reinterpret_cast<int32_t*>(base + w.stok);
-  int32_t* sid = reinterpret_cast<int32_t*>(base + w.sid);
-  int log_groups = 0;
-  while ((1 << log_groups) < kSortMinGroups || ((vocab - 1) >> log_groups) + 1 > kSortRows) ++log_groups;
+  const auto list = [&](size_t at) { return reinterpret_cast<int32_t*>(base + at); };
+  const int32_t V = static_cast<int32_t>(vocab);
   // more tokens than one sort takes: the following ones are added to the table
   for (int64_t t0 = 0; t0 < tokens; t0 += w.chunk) {
-    const int64_t n = tokens - t0 < w.chunk ? tokens - t0 : w.chunk;
-    const bool add = accumulate || t0 > 0;
-    launch_kernel(add ? dlvm_embedding_group_kernel<false> : dlvm_embedding_group_kernel<true>,
-                  dim3(1u << log_groups), dim3(kSortThreads), s, static_cast<uint32_t>(vocab), width,
-                  static_cast<int32_t>(n), log_groups, ids + t0, count, stok, sid, dtable);
+    const int32_t n = static_cast<int32_t>(tokens - t0 < w.chunk ? tokens - t0 : w.chunk);
+    const int at = sort_tokens(w, V, n, ids + t0, base, s);
+    const Chunk c{V, width, n, list(w.row[at]), list(w.tok[at]), scale, accumulate || t0 > 0,
+                  reinterpret_cast<float*>(base + w.head), reinterpret_cast<float*>(base + w.tail), dtable, w.P};
     if (dtype == F32)
-      sum_pieces_any<float>(w, width, n, base, static_cast<const float*>(dout) + t0 * width, scale, add,
-                            dtable, s);
+      sum_pieces_any<float>(c, static_cast<const float*>(dout) + t0 * width, s);
     else
-      sum_pieces_any<bf16_t>(w, width, n, base, static_cast<const bf16_t*>(dout) + t0 * width, scale, add,
-                             dtable, s);
-    const int pieces = static_cast<int>((n + w.P - 1) / w.P);
+      sum_pieces_any<bf16_t>(c, static_cast<const bf16_t*>(dout) + t0 * width, s);
+    const int pieces = (n + c.P - 1) / c.P;
     const int slabs = static_cast<int>((width + kJoinCols - 1) / kJoinCols);
     const int short_blocks = (pieces * slabs + kJoinWaves - 1) / kJoinWaves;
     launch_kernel(dlvm_embedding_join_kernel, dim3(short_blocks + pieces / kJoinLong * slabs),
-                  dim3(64 * kJoinWaves), s, width, w.P, pieces, slabs, short_blocks, count, sid, scale,
-                  add, reinterpret_cast<const float*>(base + w.head),
-                  reinterpret_cast<const float*>(base + w.tail), dtable);
+                  dim3(64 * kJoinWaves), s, V, width, c.P, pieces, slabs, short_blocks, n, c.row, scale, c.add,
+                  static_cast<const float*>(c.head), static_cast<const float*>(c.tail), dtable);
   }
   return hipGetLastError();
 }
