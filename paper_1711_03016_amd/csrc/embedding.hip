@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void dlvm_embedding_pieces_kernel(
 // are added in order. A workgroup of the second kind looks at one piece in kJoinLong,
 // so each long row is found by the first of them that lies inside it.
 // ---------------------------------------------------------------------------
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 16;
 constexpr int kJoinCols = 256;
 constexpr int kJoinLong = 8;
 
