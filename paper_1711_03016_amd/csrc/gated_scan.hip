@@ -3,17 +3,24 @@
 //
 // A step is the map h -> a h + u; maps compose, (A2, U2) after (A1, U1) being
 // (A2 A1, A2 U1 + U2), so a stretch of time is summed up by one pair of numbers for each
-// state. The adjoint is the same recurrence backwards: mu -> a (mu + dh). Every variant
-// reads its tensors once, one state to a lane (wider vectors leave fewer waves: 63
-// against 45 us with four states of bf16 to a lane, T = 32, 2^20 states):
+// state. The adjoint is the same recurrence backwards: mu -> a (mu + dh). One state to a
+// lane: wider vectors leave fewer waves (63 against 45 us with four states of bf16 to a lane,
+// T = 32, 2^20 states).
 //  - ALONE, many states or few steps: a thread takes its state through all steps;
-//  - SHARED: a workgroup takes 64 states, its eight waves equal numbers of steps of each
-//    block of time: each wave sums its steps up in registers, the sums are exchanged
-//    through LDS, and each goes through its steps again from the state before them;
-//  - SHARED in segments of time, few states and many steps: a first launch sums every
-//    segment up, and the second starts each from the sums before it. That reads half of
-//    the inputs a second time, from the Infinity Cache as far as they fit: the second
-//    launch begins with the segments that the first read last.
+//  - SHARED: a workgroup takes 64 states, its eight waves eight steps each of every 64:
+//    each wave sums its steps up in registers, the sums are exchanged through LDS, and each
+//    goes through its steps again from the state before them;
+//  - CHAINED, the forward call of few states and many steps: each block of time has a
+//    workgroup of its own, which publishes the map of its block, takes the state before it
+//    from what the workgroups of earlier blocks have published, and publishes the state
+//    after it. Every tensor is read once.
+//  - SHARED in segments of time, the gradient of few states and many steps: a first launch
+//    sums every segment up, and the second starts each from the sums after it. That reads
+//    two of five tensors a second time, from the Infinity Cache as far as they fit: the
+//    second launch begins with the segments that the first read last. (Chained, the gradient's
+//    blocks are too short for the waiting: its registers hold twelve steps of a wave, 110
+//    against 101 us for T = 4096, 8192 states of bf16, where the forward call's 32 steps take
+//    56 us chained and 74 in segments.)
 // What bounds them is memory; the arithmetic (two transcendental functions to an element)
 // takes about half of what the vector units could do in that time.
 #include <math.h>
@@ -25,10 +32,10 @@
 namespace dlvm {
 namespace {
 
-enum Mode { ALONE, SHARED };
-constexpr int kWaves = 8;   // waves of a workgroup that share the steps
-
-constexpr int kUnroll = 8;  // steps of a thread that are in flight together
+enum Mode { ALONE, SHARED, CHAINED };
+constexpr int kWaves = 8;          // waves of a workgroup that share the steps
+constexpr int kUnroll = 8;         // steps of a thread that are in flight together
+constexpr int kChainedUnroll = 32; // and in a block of a chain
 
 // a = sigmoid(z) and c = 1 - a, each to float32 accuracy on its own (1 - a from a
 // rounded a loses its digits where the gate is open). z of +-infinity gives 0 and 1, NaN
@@ -53,6 +60,111 @@ struct Cut {
   float* init;         // [N] copy of the first state (the caller's may be overwritten in place)
   float2* sums;
 };
+
+// ---------------------------------------------------------------------------
+// The chain of a CHAINED call. words[(i * tiles + tile) * 64 + lane] is, of block i of time
+// and the lane's state, first kEmpty, then the block's map (A, Q), then (kState, the state
+// after it): 64 bits that are written and read whole, so that a word needs no flag beside it
+// and no order with other memory. (A is a product of gates, never negative; a NaN is stored
+// as the one that is not kEmpty.)
+//
+// A workgroup takes the next block of its tile by a ticket, so every earlier block is
+// taken by a workgroup that runs already, and that publishes its map without waiting for
+// anything. The first block that has no state yet finds the states before it, so it goes
+// on: every wait ends. Should a workspace be used by two calls at once after all, a bound on
+// the rounds of waiting ends it with NaN. The state before a block comes from the nearest
+// earlier block whose state is known, by the maps between, applied one after the other in
+// time: the same roundings wherever the known state was found.
+// ---------------------------------------------------------------------------
+constexpr int kWindow = 64;            // earlier blocks that a workgroup looks at
+constexpr int kRounds = 1 << 17;       // about a tenth of a second
+constexpr uint32_t kEmpty = 0xffffffffu;
+constexpr float kState = -1.0f;
+constexpr int kTicketStride = 32;      // a ticket to every 128 bytes
+
+struct Chain {
+  int blocks, tiles;                   // blocks of time; workgroups of one block
+  uint32_t* tickets;
+  uint64_t* words;
+};
+
+__global__ __launch_bounds__(256) void dlvm_gated_scan_clear_kernel(Chain chain, int64_t n) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i < chain.tiles) chain.tickets[i * kTicketStride] = 0;
+  if (i < n) chain.words[i] = ~uint64_t(0);
+}
+
+typedef __attribute__((address_space(1))) uint64_t Word;
+
+// The words of a tile in block b, one to a lane: a scalar address.
+__device__ __forceinline__ Word* words_of(const Chain& chain, int tile, int b) {
+  Word* w = (Word*)chain.words + (static_cast<int64_t>(b) * chain.tiles + tile) * 64;
+  asm("" : "+s"(w));
+  return w;
+}
+
+__device__ __forceinline__ void publish(const Chain& chain, int tile, int b, int lane, float x, float y) {
+  const uint32_t hi = x != x ? 0x7fc00000u : __float_as_uint(x);
+  __hip_atomic_store(words_of(chain, tile, b) + lane, static_cast<uint64_t>(hi) << 32 | __float_as_uint(y),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The state before block i (> 0) of the lane's state. All waves of the workgroup call it.
+__device__ __forceinline__ float state_before(const Chain& chain, int tile, int i, int wave, int lane,
+                                              uint64_t (*window)[64]) {
+  constexpr int each = kWindow / kWaves;
+  const auto ready = [](uint64_t m) { return static_cast<uint32_t>(m >> 32) != kEmpty; };
+  const auto state = [](uint64_t m) { return static_cast<uint32_t>(m >> 32) == __float_as_uint(kState); };
+  const auto load = [&](int b) {
+    return b >= 0 ? __hip_atomic_load(words_of(chain, tile, b) + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                  : static_cast<uint64_t>(__float_as_uint(kState)) << 32;
+  };
+  int look = kWaves;  // the nearest blocks first: a block's words are as many bytes as a step's inputs
+#pragma unroll 1
+  for (int round = 0; round < kRounds; ++round) {
+    if (look == kWaves) {
+      window[wave][lane] = load(i - 1 - wave);
+    } else {
+      uint64_t m[each];
+#pragma unroll
+      for (int e = 0; e < each; ++e) m[e] = load(i - 1 - (wave * each + e));
+#pragma unroll
+      for (int e = 0; e < each; ++e) window[wave * each + e][lane] = m[e];
+    }
+    __syncthreads();
+    // how far back every lane finds a state, with no gap before it
+    int far = 0;
+    bool found = false, gap = false;
+#pragma unroll 1
+    while (far < look) {
+#pragma unroll 4
+      for (int e = 0; e < each; ++e) {
+        const uint64_t v = window[far + e][lane];
+        gap = gap || (!found && !ready(v));
+        found = found || state(v);
+      }
+      far += each;
+      if (__ballot(gap) != 0 || __ballot(found) == ~uint64_t(0)) break;
+    }
+    const bool whole = __ballot(gap) == 0;
+    const bool done = whole && __ballot(found) == ~uint64_t(0);
+    float h = 0.0f;
+    if (done) {
+#pragma unroll 4
+      for (int k = far - 1; k >= 0; --k) {
+        const uint64_t v = window[k][lane];
+        const float A = __uint_as_float(static_cast<uint32_t>(v >> 32));
+        const float Q = __uint_as_float(static_cast<uint32_t>(v));
+        h = state(v) ? Q : fmaf(A, h, Q);
+      }
+    }
+    __syncthreads();
+    if (done) return h;
+    if (whole) look = kWindow;
+    else __builtin_amdgcn_s_sleep(1);
+  }
+  return NAN;
+}
 
 // Of a thread: whether it has a state, which, and the state's batch entry and column;
 // b0 and c0 are those of the wave's first lane. (A lane without a state has the first's.)
@@ -103,30 +215,48 @@ __device__ __forceinline__ int32_t wave_max(int32_t v) {
   return __builtin_amdgcn_readfirstlane(v);
 }
 
+// The block of time and the tile of states of a workgroup (and, ALONE, of a wave).
+template <int MODE>
+__device__ __forceinline__ void work_of(const Chain& chain, int wave, int& block, int& tile) {
+  if (MODE == CHAINED) {
+    __shared__ uint32_t taken;
+    tile = static_cast<int>(blockIdx.x % static_cast<uint32_t>(chain.tiles));
+    if (threadIdx.x == 0)
+      taken = __hip_atomic_fetch_add(chain.tickets + tile * kTicketStride, 1u, __ATOMIC_RELAXED,
+                                     __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const uint32_t next = __builtin_amdgcn_readfirstlane(taken);
+    block = next < static_cast<uint32_t>(chain.blocks) ? static_cast<int>(next) : chain.blocks;
+  } else {
+    block = 0;
+    tile = static_cast<int>(blockIdx.x) * (MODE == ALONE ? 4 : 1) + (MODE == ALONE ? wave : 0);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Forward.
 // ---------------------------------------------------------------------------
 template <typename E, bool COUPLED, int MODE>
-__global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_scan_kernel(GatedScan k, Cut cut) {
-  constexpr int U = kUnroll, NW = MODE == ALONE ? 1 : kWaves;
-  __shared__ float2 sums[2][NW][MODE == ALONE ? 1 : 64];
+__global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_scan_kernel(GatedScan k, Chain chain) {
+  constexpr int U = MODE == CHAINED ? kChainedUnroll : kUnroll, NW = MODE == ALONE ? 1 : kWaves;
+  __shared__ float2 sums[MODE == SHARED ? 2 : 1][MODE == ALONE ? 1 : NW][MODE == ALONE ? 1 : 64];
+  __shared__ uint64_t window[MODE == CHAINED ? kWindow : 1][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
   const int w = MODE == ALONE ? 0 : wave;
-  const int block = static_cast<int>(blockIdx.x) % cut.tiles;
-  const int s = cut.S - 1 - static_cast<int>(blockIdx.x) / cut.tiles;
-  const Place p = place_of(MODE == ALONE ? block * 4 + wave : block, lane, k);
+  int block, tile;
+  work_of<MODE>(chain, wave, block, tile);
+  if (MODE == CHAINED && block >= chain.blocks) return;
+  const Place p = place_of(tile, lane, k);
   if (MODE == ALONE && !p.on) return;
-  const int64_t N = k.B * k.H;
+  const int32_t begin = block * (NW * U);
   const int32_t T = static_cast<int32_t>(k.T);
-  const int32_t begin = s * cut.len;
-  const int32_t end = T - begin < cut.len ? T : begin + cut.len;
+  const int32_t end = MODE != CHAINED || T - begin < NW * U ? T : begin + NW * U;
   const int32_t n = length_of(k.lens, p.b, k.T);
   const int32_t live = !p.on ? 0 : n < end ? n : end;  // steps below it are read
   const Rows<E> pz(k.z, k.ldz, k.B, p), px(k.x, k.ldx, k.B, p), ph(k.hs, k.ldh, k.B, p);
 
-  const float* first = cut.S > 1 ? cut.init : k.h0;
-  float h = first != nullptr ? first[p.j] : 0.0f;
+  float h = k.h0 != nullptr && block == 0 ? k.h0[p.j] : 0.0f;
   E z[U] = {}, x[U] = {};
   // Loads without conditions, steps behind the last that is live in any lane from that
   // one: in a branch of its own each load would be waited for before the next is sent.
@@ -146,10 +276,6 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   };
   fetch(begin + w * U);
   asm volatile("" : "+v"(h));  // every wave has its first state before one can write hT over it
-  for (int q = 0; q < s; ++q) {
-    const float2 m = cut.sums[q * N + p.j];
-    h = fmaf(m.x, h, m.y);
-  }
 
   int phase = 0;
   for (int32_t t0 = begin; t0 < end; t0 += NW * U) {
@@ -170,9 +296,9 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
           a[u] = 1.0f;
           q[u] = 0.0f;
         }
-    fetch(t + NW * U);
+    if (MODE != CHAINED) fetch(t + NW * U);
     float now = h;
-    if (MODE == SHARED) {
+    if (MODE != ALONE) {
       float A = a[0], Q = q[0];
 #pragma unroll
       for (int u = 1; u < U; ++u) {
@@ -194,9 +320,14 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
         Q = fmaf(m.x, Q, m.y);
         A *= m.x;
       }
+      if (MODE == CHAINED && block > 0) {
+        if (w == 0) publish(chain, tile, block, lane, A, Q);
+        h = state_before(chain, tile, block, wave, lane, window);
+      }
       now = fmaf(Aw, h, Qw);
-      h = fmaf(A, h, Q);
-      phase ^= 1;
+      h = fmaf(A, h, Q);  // as state_before finds it from the map
+      if (MODE == CHAINED && w == 0) publish(chain, tile, block, lane, kState, h);
+      if (MODE == SHARED) phase ^= 1;
     }
     auto rh = ph.row(t);
     if (whole && p.on) {
@@ -213,6 +344,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
       }
     }
     if (MODE == ALONE) h = now;
+    if (MODE == CHAINED) break;  // a block is one round
   }
   if (k.hT != nullptr && p.on && w == 0 && end == T) k.hT[p.j] = h;
 }
@@ -274,14 +406,15 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   int phase = 0;
   for (int32_t t0 = last; t0 >= begin; t0 -= NW * U) {
     const int32_t t = t0 + w * U;
-    float a[U], c[U], xs[U], hp[U], dh[U];
-    hp[0] = t > 0 ? load_as_f32(&before) : k.h0 != nullptr ? k.h0[p.j] : 0.0f;
+    float a[U], c[U], f[U], dh[U];  // f: dz over the adjoint that passes the gate
+    float prev = t > 0 ? load_as_f32(&before) : k.h0 != nullptr ? k.h0[p.j] : 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       gate(load_as_f32(&z[u]), a[u], c[u]);
-      xs[u] = load_as_f32(&x[u]);
+      const float xv = load_as_f32(&x[u]);
       dh[u] = load_as_f32(&d[u]);
-      if (u + 1 < U) hp[u + 1] = a[u] * hp[u] + (COUPLED ? c[u] * xs[u] : xs[u]);
+      f[u] = (COUPLED ? prev - xv : prev) * c[u];
+      prev = a[u] * prev + (COUPLED ? c[u] * xv : xv);
     }
     const bool whole = k.lens == nullptr && has_d && t + U <= end;  // every step is live
     if (!whole)
@@ -324,7 +457,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
       for (int u = U - 1; u >= 0; --u, rz -= gz.step, rx -= gx.step) {
         const float lam = now + dh[u];
         now = a[u] * lam;
-        gz.in(rz) = store_cast<E>((COUPLED ? hp[u] - xs[u] : hp[u]) * c[u] * now);
+        gz.in(rz) = store_cast<E>(f[u] * now);
         gx.in(rx) = store_cast<E>(COUPLED ? c[u] * lam : lam);
       }
     } else {
@@ -334,7 +467,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
         now = a[u] * lam;
         const bool in = t + u < live;
         if (p.on && t + u < end) {
-          gz.in(rz) = store_cast<E>(in ? (COUPLED ? hp[u] - xs[u] : hp[u]) * c[u] * now : 0.0f);
+          gz.in(rz) = store_cast<E>(in ? f[u] * now : 0.0f);
           gx.in(rx) = store_cast<E>(in ? (COUPLED ? c[u] * lam : lam) : 0.0f);
         }
       }
@@ -345,72 +478,62 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
 }
 
 // ---------------------------------------------------------------------------
-// The map of each segment: the waves take equal stretches of it, whose maps are composed
-// in order. ADJOINT: of the gradient, backwards in time (the stretches are read
-// forwards, the last wave's applied first).
+// The map of each segment of the gradient but the first, of the adjoint after it to that
+// before it: the waves take equal stretches of it (read forwards), whose maps are composed
+// from the last.
 // ---------------------------------------------------------------------------
-template <typename E, bool COUPLED, bool ADJOINT>
+template <typename E>
 __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(GatedScan k, Cut cut) {
   constexpr int U = 2 * kUnroll;
   __shared__ float2 sums[kWaves][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  // the forward call needs no map of the last segment, the gradient none of the first
-  const int s = static_cast<int>(blockIdx.x) / cut.tiles + (ADJOINT ? 1 : 0);
+  const int s = static_cast<int>(blockIdx.x) / cut.tiles + 1;
   const Place p = place_of(static_cast<int>(blockIdx.x) % cut.tiles, lane, k);
   const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;
   const int32_t end = T - begin < cut.len ? T : begin + cut.len;
   const int32_t n = length_of(k.lens, p.b, k.T);
-  const bool has_u = !ADJOINT || k.dhs != nullptr;
+  const bool has_d = k.dhs != nullptr;
   const Rows<E> pz(k.z, k.ldz, k.B, p);
-  const Rows<E> pu(!ADJOINT ? k.x : has_u ? k.dhs : k.z, !ADJOINT ? k.ldx : has_u ? k.lddh : k.ldz, k.B, p);
-  if (p.on && wave == 0 && s == (ADJOINT ? cut.S - 1 : 0)) {
-    const float* first = ADJOINT ? k.dhT : k.h0;
-    cut.init[p.j] = first != nullptr ? first[p.j] : 0.0f;
-  }
+  const Rows<E> pd(has_d ? k.dhs : k.z, has_d ? k.lddh : k.ldz, k.B, p);
+  if (p.on && wave == 0 && s == cut.S - 1) cut.init[p.j] = k.dhT != nullptr ? k.dhT[p.j] : 0.0f;
 
   const int32_t stretch = (cut.len + kWaves * U - 1) / (kWaves * U) * U;
   const int32_t t_begin = begin + wave * stretch;
   const int32_t t_end = t_begin + stretch < end ? t_begin + stretch : end;
   const int32_t live = !p.on ? 0 : n < t_end ? n : t_end;
   const int32_t t_live = k.lens == nullptr ? t_end : wave_max(live);  // no step is live in any lane beyond
-  float A = 1.0f, Q = 0.0f;
+  float A = 1.0f, M = 0.0f;
   for (int32_t t0 = t_begin; t0 < t_live; t0 += U) {
-    E z[U], v[U];
-    auto rz = pz.row(t0), ru = pu.row(t0);
+    E z[U], d[U];
+    auto rz = pz.row(t0), rd = pd.row(t0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       z[u] = pz.in(rz);
-      v[u] = pu.in(ru);
+      d[u] = pd.in(rd);
       const bool more = t0 + u + 1 < t_live;
       rz += more ? pz.step : 0;
-      ru += more ? pu.step : 0;
+      rd += more ? pd.step : 0;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float a, c;
       gate(load_as_f32(&z[u]), a, c);
-      float q = has_u ? load_as_f32(&v[u]) : 0.0f;
+      const float dh = has_d ? load_as_f32(&d[u]) : 0.0f;
       const bool in = t0 + u < live;
-      if (ADJOINT) {
-        // the adjoint of step t reaches the state before the stretch through the gates up to its own
-        A = in ? A * a : A;
-        Q = in ? fmaf(A, q, Q) : Q;
-      } else {
-        q = COUPLED ? c * q : q;
-        Q = in ? fmaf(a, Q, q) : Q;
-        A = in ? A * a : A;
-      }
+      // the adjoint of a step reaches the state before the stretch through the gates up to its own
+      A = in ? A * a : A;
+      M = in ? fmaf(A, dh, M) : M;
     }
   }
-  sums[wave][lane] = make_float2(A, Q);
+  sums[wave][lane] = make_float2(A, M);
   __syncthreads();
   if (wave == 0 && p.on) {
     float2 m = make_float2(1.0f, 0.0f);
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      const float2 o = sums[ADJOINT ? kWaves - 1 - i : i][lane];
+    for (int i = kWaves - 1; i >= 0; --i) {
+      const float2 o = sums[i][lane];
       m = make_float2(o.x * m.x, fmaf(o.x, m.y, o.y));
     }
     cut.sums[s * (k.B * k.H) + p.j] = m;
@@ -419,18 +542,24 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
 
 // ---------------------------------------------------------------------------
 // Choice of the variant, for N states: alone where a thread to each state fills the GPU
-// (sixteen waves on a compute unit) or there are no steps to share; in segments where the
-// tiles of states are so few that the second reading costs less than the idle units:
-// T 4096, 128 tiles of bf16, forward and gradient 267 us in one piece, 176 in four segments;
-// T 777, 204 tiles of float32, 85-91 in one piece, 92 in three.
+// (sixteen waves on a compute unit) or there are no steps to share; chained, or in segments,
+// where the tiles of states leave compute units idle for so many steps that it pays for
+// another launch and the waiting, or the second reading. Forward, bf16, in one piece against
+// chained: 8 tiles, T 1024 20.8 and 9.5 us, T 16384 295 and 21; 128 tiles, T 1024 22 and 16,
+// T 4096 76 and 44; 188 tiles, T 1024 24 and 27, T 2048 43 and 43. Gradient: 128 tiles, T 4096
+// 167 in one piece, 101 in four segments; 204 tiles of float32, T 777 56 and 50 in three.
 // ---------------------------------------------------------------------------
 constexpr int64_t kBlocks = 512;       // two workgroups on a compute unit
-constexpr int64_t kUncut = 192;        // tiles from which the second reading costs more than it gives
+constexpr int64_t kUncut = 192;        // tiles from which a gradient is not cut
+constexpr int64_t kUnchained = 160;    // and a forward call not chained
 constexpr int32_t kShortest = 128;     // steps of a segment at least
 
 bool alone(int64_t T, int64_t N) { return T <= 2 * kUnroll || (N + 63) / 64 >= 4096; }
+bool chained(int64_t T, int64_t N) {
+  return !alone(T, N) && (N + 63) / 64 < kUnchained && T >= 2 * kWaves * kChainedUnroll;
+}
 
-// Segments of a call, and the steps of one.
+// Segments of a gradient, and the steps of one.
 int segments(int64_t T, int64_t N, int32_t* len) {
   const int64_t tiles = (N + 63) / 64, step = kWaves * kUnroll;
   int64_t S = alone(T, N) || tiles >= kUncut ? 1 : (kBlocks + tiles - 1) / tiles;
@@ -441,16 +570,36 @@ int segments(int64_t T, int64_t N, int32_t* len) {
   return static_cast<int>((T + L - 1) / L);
 }
 
-template <typename E, bool COUPLED, bool GRAD>
-hipError_t run(const GatedScan& c, void* ws, hipStream_t s) {
+int blocks_of(int64_t T) {
+  constexpr int steps = kWaves * kChainedUnroll;
+  return static_cast<int>((T + steps - 1) / steps);
+}
+
+template <typename E, bool COUPLED> hipError_t forward(const GatedScan& c, void* ws, hipStream_t s) {
+  const int64_t N = c.B * c.H;
+  Chain chain{1, static_cast<int>((N + 63) / 64), nullptr, nullptr};
+  if (alone(c.T, N)) {
+    launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, ALONE>, dim3((chain.tiles + 3) / 4), dim3(256), s, c, chain);
+  } else if (ws == nullptr || !chained(c.T, N)) {
+    launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, SHARED>, dim3(chain.tiles), dim3(64 * kWaves), s, c, chain);
+  } else {
+    chain.blocks = blocks_of(c.T);
+    chain.tickets = static_cast<uint32_t*>(ws);
+    chain.words = reinterpret_cast<uint64_t*>(chain.tickets + chain.tiles * kTicketStride);
+    const int64_t n = static_cast<int64_t>(chain.blocks) * chain.tiles * 64;
+    launch_kernel(dlvm_gated_scan_clear_kernel, dim3(static_cast<uint32_t>((n + 255) / 256)), dim3(256), s, chain, n);
+    launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, CHAINED>, dim3(chain.tiles * chain.blocks),
+                  dim3(64 * kWaves), s, c, chain);
+  }
+  return hipGetLastError();
+}
+
+template <typename E, bool COUPLED> hipError_t backward(const GatedScan& c, void* ws, hipStream_t s) {
   const int64_t N = c.B * c.H;
   Cut cut{1, static_cast<int32_t>(c.T), static_cast<int>((N + 63) / 64), nullptr, nullptr};
   if (alone(c.T, N)) {
     cut.tiles = (cut.tiles + 3) / 4;
-    if constexpr (GRAD)
-      launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, ALONE>, dim3(cut.tiles), dim3(256), s, c, cut);
-    else
-      launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, ALONE>, dim3(cut.tiles), dim3(256), s, c, cut);
+    launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, ALONE>, dim3(cut.tiles), dim3(256), s, c, cut);
     return hipGetLastError();
   }
   const dim3 block(64 * kWaves);
@@ -458,18 +607,10 @@ hipError_t run(const GatedScan& c, void* ws, hipStream_t s) {
   if (cut.S > 1) {
     cut.init = static_cast<float*>(ws);
     cut.sums = reinterpret_cast<float2*>(cut.init + (N + 63) / 64 * 64);
-    launch_kernel(dlvm_gated_scan_sums_kernel<E, COUPLED, GRAD>, dim3(cut.tiles * (cut.S - 1)), block, s, c, cut);
+    launch_kernel(dlvm_gated_scan_sums_kernel<E>, dim3(cut.tiles * (cut.S - 1)), block, s, c, cut);
   }
-  if constexpr (GRAD)
-    launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, SHARED>, dim3(cut.tiles * cut.S), block, s, c, cut);
-  else
-    launch_kernel(dlvm_gated_scan_kernel<E, COUPLED, SHARED>, dim3(cut.tiles * cut.S), block, s, c, cut);
+  launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, SHARED>, dim3(cut.tiles * cut.S), block, s, c, cut);
   return hipGetLastError();
-}
-
-template <bool GRAD> hipError_t run_any(const GatedScan& c, void* ws, hipStream_t s) {
-  return c.dtype == F32 ? (c.coupled ? run<float, true, GRAD>(c, ws, s) : run<float, false, GRAD>(c, ws, s))
-                        : (c.coupled ? run<bf16_t, true, GRAD>(c, ws, s) : run<bf16_t, false, GRAD>(c, ws, s));
 }
 
 }  // namespace
@@ -477,15 +618,23 @@ template <bool GRAD> hipError_t run_any(const GatedScan& c, void* ws, hipStream_
 size_t gated_scan_ws(int, int64_t T, int64_t B, int64_t H) {
   int32_t len = 0;
   const int64_t N = B * H, S = segments(T, N, &len);
-  return S == 1 ? 256 : static_cast<size_t>((N + 63) / 64 * 64) * 4 + static_cast<size_t>(S) * N * 8;
+  const size_t tiles = static_cast<size_t>((N + 63) / 64);
+  size_t bytes = S == 1 ? 256 : tiles * 64 * 4 + static_cast<size_t>(S) * N * 8;
+  if (chained(T, N)) {
+    const size_t chain = tiles * (kTicketStride * 4 + static_cast<size_t>(blocks_of(T)) * 64 * 8);
+    bytes = chain > bytes ? chain : bytes;
+  }
+  return bytes;
 }
 
 hipError_t launch_gated_scan_forward(const GatedScan& c, void* ws, hipStream_t s) {
-  return run_any<false>(c, ws, s);
+  if (c.dtype == F32) return (c.coupled ? forward<float, true> : forward<float, false>)(c, ws, s);
+  return (c.coupled ? forward<bf16_t, true> : forward<bf16_t, false>)(c, ws, s);
 }
 
 hipError_t launch_gated_scan_backward(const GatedScan& c, void* ws, hipStream_t s) {
-  return run_any<true>(c, ws, s);
+  if (c.dtype == F32) return (c.coupled ? backward<float, true> : backward<float, false>)(c, ws, s);
+  return (c.coupled ? backward<bf16_t, true> : backward<bf16_t, false>)(c, ws, s);
 }
 
 }  // namespace dlvm

@@ -192,7 +192,29 @@ def test_optional_arguments(dtype, size, which):
     _compare(_run(T, B, H, dtype, "coupled", z, x, h0, None, dhs, dhT), ref, tol)
 
 
-@pytest.mark.parametrize("T", [1, 40, 900])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mode", ["free", "coupled"])
+@pytest.mark.parametrize("size,ragged", [((40000, 1, 70), False), ((20011, 3, 64), True), ((1024, 190, 64), False)])
+def test_long_sequences(dtype, mode, size, ragged):
+    """More blocks of time than a workgroup looks at once, and the same bits every time."""
+    T, B, H = size
+    z, x, h0, dhs, dhT, lens = _case(T, B, H, dtype, ragged, False, 9)
+    z += 3.0                                            # gates so open that states reach far
+    q = [quant(v, dtype) for v in (z, x, dhs)]
+    h, _ = oracle.gated_scan(q[0], q[1], h0, lens, mode == "coupled")
+    tol = _bounds(q[0], q[1], h0, lens, mode == "coupled", q[2], dhT, dtype)
+    got = _run(T, B, H, dtype, mode, z, x, h0, lens, dhs, dhT)
+    live = np.arange(T)[:, None] < (np.full(B, T) if lens is None else np.clip(lens, 0, T))
+    _compare(got, {"hs": np.where(live[..., None], h[1:], 0.0), "hT": h[-1]}, tol)
+    whole = _run(T, B, H, dtype, mode, z, x, h0, lens, dhs, dhT, use_ws=False)
+    # a gradient in one piece is within the bound of the oracle's (above): this one of it
+    _compare(got, {k: whole[k] for k in ("dz", "dx", "dh0")}, {k: 2 * v for k, v in tol.items()})
+    for _ in range(3):
+        again = _run(T, B, H, dtype, mode, z, x, h0, lens, dhs, dhT)
+        assert all((again[k] == got[k]).all() for k in got)
+
+
+@pytest.mark.parametrize("T", [1, 40, 900, 1500])
 def test_state_in_place_and_in_pieces(T):
     """hT may be h0 and dh0 may be dhT: a sequence fed in pieces through one state."""
     import torch
