@@ -240,16 +240,41 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
     }
 }
 
-__global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(int32_t V, int32_t N, int bits, int digit_bits,
-                                                                           const int32_t* __restrict__ ids,
-                                                                           int32_t* __restrict__ row_out,
-                                                                           int32_t* __restrict__ tok_out) {
+// One row of zeros by a wave.
+__device__ __forceinline__ void zero_row(float* __restrict__ row, int64_t E) {
+  using Quad = Elems<float, 4>;
+  const Quad zero{{0.0f, 0.0f, 0.0f, 0.0f}};
+  int64_t c = 4 * (threadIdx.x & 63);
+  for (; c + 4 <= E; c += 256) *reinterpret_cast<Quad*>(row + c) = zero;
+  for (; c < E; ++c) row[c] = 0.0f;
+}
+
+// The first workgroup sorts; each of the others zeroes the absent ones of `share` rows, which it
+// finds by reading all ids.
+__global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
+    int32_t V, int64_t E, int32_t N, int bits, int digit_bits, int share, const int32_t* __restrict__ ids,
+    int32_t* __restrict__ row_out, int32_t* __restrict__ tok_out, float* __restrict__ dtable) {
   constexpr int W = kSmallSort / kSortThreads;
   __shared__ int32_t places[kSortWaves][kDigits];
   __shared__ int32_t rows[kSmallSort];
   __shared__ uint16_t toks[kSmallSort];
   __shared__ int32_t sums[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x > 0) {
+    uint8_t* present = reinterpret_cast<uint8_t*>(places);
+    const int32_t r0 = static_cast<int32_t>(blockIdx.x - 1) * share;
+    const int32_t n = V - r0 < share ? V - r0 : share;
+    for (int r = tid; r < n; r += kSortThreads) present[r] = 0;
+    __syncthreads();
+    for (int32_t i = tid; i < N; i += kSortThreads) {
+      const uint32_t r = static_cast<uint32_t>(ids[i]) - static_cast<uint32_t>(r0);
+      if (r < static_cast<uint32_t>(n)) present[r] = 1;
+    }
+    __syncthreads();
+    for (int r = wave; r < n; r += kSortWaves)
+      if (present[r] == 0) zero_row(dtable + static_cast<int64_t>(r0 + r) * E, E);
+    return;
+  }
   const int span = (N + kSortThreads - 1) / kSortThreads * 64;  // tokens of a wave
   const int first = wave * span + lane;
   int32_t row[W], tok[W], digit[W], rank[W];
@@ -307,7 +332,6 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(int32
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void zero_absent(int32_t V, int64_t E, int32_t N, int64_t first,
                                             const int32_t* __restrict__ sid, float* __restrict__ dtable) {
-  using Quad = Elems<float, 4>;
   const int lane = threadIdx.x & 63;
   const int64_t v = first + lane;
   int32_t lo = 0, hi = N;  // the first place that holds v or more
@@ -317,13 +341,8 @@ __device__ __forceinline__ void zero_absent(int32_t V, int64_t E, int32_t N, int
     else hi = mid;
   }
   const bool absent = v < V && !(lo < N && sid[lo] == v);
-  const Quad zero{{0.0f, 0.0f, 0.0f, 0.0f}};
-  for (uint64_t todo = __ballot(absent); todo != 0; todo &= todo - 1) {
-    float* row = dtable + (first + __builtin_ctzll(todo)) * E;
-    int64_t c = 4 * lane;
-    for (; c + 4 <= E; c += 256) *reinterpret_cast<Quad*>(row + c) = zero;
-    for (; c < E; ++c) row[c] = 0.0f;
-  }
+  for (uint64_t todo = __ballot(absent); todo != 0; todo &= todo - 1)
+    zero_row(dtable + (first + __builtin_ctzll(todo)) * E, E);
 }
 
 template <int VEC, int G>
@@ -574,15 +593,22 @@ GradWs grad_ws(int64_t width, int64_t tokens) {
   return w;
 }
 
-// The call's n tokens sorted by row; returns which of the two lists holds them.
-int sort_tokens(const GradWs& w, int32_t V, int32_t n, const int32_t* ids, char* ws, hipStream_t s) {
+// The call's n tokens sorted by row; returns which of the two lists holds them. A sort by one
+// workgroup leaves the GPU to others that zero the rows without a token (`zero`).
+int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t* ids, char* ws, bool zero,
+                float* dtable, hipStream_t s) {
   const auto list = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
   int bits = 1;  // of the largest key, V
   while ((V >> bits) != 0) ++bits;
   const int passes = (bits + kDigitBits - 1) / kDigitBits, digit_bits = (bits + passes - 1) / passes;
   if (n <= kSmallSort) {
-    launch_kernel(dlvm_embedding_sort_kernel, dim3(1), dim3(kSortThreads), s, V, n, bits, digit_bits, ids,
-                  list(w.row[0]), list(w.tok[0]));
+    // a workgroup to each other compute unit, of 64 rows at least and those it can mark at most
+    constexpr int marks = sizeof(int32_t) * kSortWaves * kDigits;
+    const int even = (V + 254) / 255;
+    const int share = even < 64 ? 64 : even < marks ? even : marks;
+    const uint32_t others = zero ? static_cast<uint32_t>((V + share - 1) / share) : 0;
+    launch_kernel(dlvm_embedding_sort_kernel, dim3(1 + others), dim3(kSortThreads), s, V, E, n, bits,
+                  digit_bits, share, ids, list(w.row[0]), list(w.tok[0]), dtable);
     return 0;
   }
   const dim3 blocks(static_cast<uint32_t>((n + kSortBlock - 1) / kSortBlock));
@@ -622,7 +648,7 @@ struct Chunk {
   int32_t n;
   const int32_t *row, *tok;
   float scale;
-  bool add;
+  bool add, zero;  // added to the table; whether rows without a token are still to be zeroed
   float *head, *tail, *dtable;
   int P;
 };
@@ -630,7 +656,7 @@ struct Chunk {
 template <typename T, int VEC, int G>
 void sum_pieces(const Chunk& c, const T* dout, hipStream_t s) {
   const int64_t pieces = (c.n + c.P - 1) / c.P, slabs = (c.E + 64 * VEC * G - 1) / (64 * VEC * G);
-  const int64_t sum_blocks = (pieces * slabs + 3) / 4, zero_blocks = c.add ? 0 : (c.V + 255) / 256;
+  const int64_t sum_blocks = (pieces * slabs + 3) / 4, zero_blocks = c.zero ? (c.V + 255) / 256 : 0;
   launch_kernel(dlvm_embedding_pieces_kernel<T, VEC, G>, dim3(static_cast<uint32_t>(sum_blocks + zero_blocks)),
                 dim3(256), s, c.V, c.E, c.P, static_cast<int>(pieces), static_cast<int>(slabs),
                 static_cast<int>(sum_blocks), c.n, c.tok, c.row, dout, c.scale, c.add, c.head, c.tail, c.dtable);
@@ -673,8 +699,9 @@ hipError_t launch_embedding_backward(int dtype, int64_t vocab, int64_t width, in
   // more tokens than one sort takes: the following ones are added to the table
   for (int64_t t0 = 0; t0 < tokens; t0 += w.chunk) {
     const int32_t n = static_cast<int32_t>(tokens - t0 < w.chunk ? tokens - t0 : w.chunk);
-    const int at = sort_tokens(w, V, n, ids + t0, base, s);
-    const Chunk c{V, width, n, list(w.row[at]), list(w.tok[at]), scale, accumulate || t0 > 0,
+    const bool add = accumulate || t0 > 0;
+    const int at = sort_tokens(w, V, width, n, ids + t0, base, !add, dtable, s);
+    const Chunk c{V, width, n, list(w.row[at]), list(w.tok[at]), scale, add, !add && n > kSmallSort,
                   reinterpret_cast<float*>(base + w.head), reinterpret_cast<float*>(base + w.tail), dtable, w.P};
     if (dtype == F32)
       sum_pieces_any<float>(c, static_cast<const float*>(dout) + t0 * width, s);
@@ -683,6 +710,7 @@ hipError_t launch_embedding_backward(int dtype, int64_t vocab, int64_t width, in
     const int pieces = (n + c.P - 1) / c.P;
     const int slabs = static_cast<int>((width + kJoinCols - 1) / kJoinCols);
     const int short_blocks = (pieces * slabs + kJoinWaves - 1) / kJoinWaves;
+    if (pieces == 1) continue;  // nothing runs over its end
     launch_kernel(dlvm_embedding_join_kernel, dim3(short_blocks + pieces / kJoinLong * slabs),
                   dim3(64 * kJoinWaves), s, V, width, c.P, pieces, slabs, short_blocks, n, c.row, scale, c.add,
                   static_cast<const float*>(c.head), static_cast<const float*>(c.tail), dtable);
