@@ -472,7 +472,7 @@ dlvm_status dlvm_sgd(int32_t dtype, int64_t n, void* params, float* master,
  * width] are `dtype`; the product with `scale` is float32, rounded once. A row
  * whose id is -1 is zero; one whose id is any other value outside [0, vocab)
  * is NaN. vocab at most 2^24, width at most 2^20, tokens at most 2^30, scale
- * finite. */
+ * finite; out must not overlap the table. */
 dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
                                    const void* table, const int32_t* ids, float scale, void* out,
                                    void* stream);
@@ -484,8 +484,8 @@ dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, 
  * touched (a table shared with the output layer, several batches to a step).
  * Ids outside [0, vocab) contribute nothing. Tokens are sorted by id first and
  * a row is summed in an order and in parts that depend on the ids alone: no
- * floating-point atomics. `ws` needs
- * dlvm_embedding_backward_ws_bytes (0 for invalid sizes). */
+ * floating-point atomics. `ws` needs dlvm_embedding_backward_ws_bytes (0 for
+ * invalid sizes). */
 size_t dlvm_embedding_backward_ws_bytes(int64_t vocab, int64_t width, int64_t tokens);
 dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
                                     const int32_t* ids, const void* dout, float scale,
@@ -525,7 +525,8 @@ dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, 
  * it (the states between are recomputed from a few of its rows). Writes dz and
  * dx (strides lddz, lddx, `dtype`; they may be the two halves of one buffer)
  * and, unless NULL, dh0 (float32 [batch, width]; it may be dhT). Rows t >=
- * lens[b] of dz and dx are zero; those of dhs are not used. */
+ * lens[b] of dz and dx are zero; those of dhs are not used. Outputs must not
+ * overlap inputs otherwise. */
 dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps, int64_t batch,
                                      int64_t width, const void* z, int64_t ldz, const void* x,
                                      int64_t ldx, const float* h0, const int32_t* lens,
@@ -547,9 +548,9 @@ dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps,
  *               at most classes; 0: both NULL.
  * Classes masked with -infinity (or the type's lowest value) have probability
  * 0 and no part in the entropy. A row whose y are all below -1e30 is masked
- * everywhere: it has lse = logp = top_logp = -infinity and entropy 0. A row with a NaN or +infinity has NaN for
- * lse, logp, entropy and top_logp; a NaN counts as -infinity in the order of
- * top_ids. `ws` (dlvm_token_logprobs_ws_bytes, or NULL) lets a call of few
+ * everywhere: it has lse = logp = top_logp = -infinity and entropy 0. A row
+ * with a NaN or +infinity has NaN for lse, logp, entropy and top_logp; a NaN
+ * counts as -infinity in the order of top_ids. `ws` (dlvm_token_logprobs_ws_bytes, or NULL) lets a call of few
  * rows cut them into parts that run side by side; with NULL no row is cut. */
 enum { DLVM_TOP_MAX = 32 };
 size_t dlvm_token_logprobs_ws_bytes(int64_t rows, int64_t classes, int32_t top);
@@ -566,8 +567,9 @@ dlvm_status dlvm_token_logprobs(int32_t dtype, int64_t rows, int64_t classes, co
  * stride ld_out, columns classes .. ld_out not touched. lse (and entropy, with
  * dentropy) as dlvm_token_logprobs wrote them for the same logits and scale.
  * Rows whose token is -1 (tokens may be NULL without dlogp) take no part of
- * dlogp; rows whose token is any other value outside [0, classes) are NaN with
- * dlogp given. A row masked everywhere has a zero gradient. Probabilities are
+ * dlogp, and where their dentropy is zero or NULL too, their gradient is zero
+ * whatever their logits hold; rows whose token is any other value outside
+ * [0, classes) are NaN with dlogp given. A row masked everywhere has a zero gradient. Probabilities are
  * exp(y - lse), off by half a step of lse. dlogits may be the logits themselves
  * (same type and stride), overwritten in place. */
 dlvm_status dlvm_token_logprobs_backward(int32_t dtype, int32_t out_dtype, int64_t rows,

@@ -136,6 +136,6 @@ def token_scores_vjp(logits, tokens, scale, dlogp, dentropy):
             hot = np.zeros(V)
             hot[t] = 1.0
             d[i] += dlogp[i] * (hot - p)
-        if dentropy is not None:
+        if dentropy is not None and dentropy[i] != 0:  # a row without adjoints is zero
             d[i] -= dentropy[i] * np.where(p > 0, p * (np.where(p > 0, lp, 0.0) + ent), 0.0)
     return d * scale

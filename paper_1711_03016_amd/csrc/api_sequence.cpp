@@ -63,6 +63,11 @@ dlvm_status score_sizes(int32_t dtype, int64_t rows, int64_t classes, int64_t ld
 
 template <typename... P> bool all_aligned16(const P*... p) { return (aligned16(p) && ...); }
 
+// Whether `out` starts where one of the inputs does.
+template <typename... P> bool is_one_of(const void* out, const P*... in) { return ((out == in) || ...); }
+
+dlvm_status overlap() { return fail(DLVM_ERR_INVALID_ARG, "an output must not overlap an input or another output"); }
+
 dlvm_status misaligned() {
   return fail(DLVM_ERR_MISALIGNED, "device pointers must be 16-byte aligned");
 }
@@ -79,6 +84,7 @@ dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, 
   if (table == nullptr || ids == nullptr || out == nullptr)
     return fail(DLVM_ERR_INVALID_ARG, "null argument");
   if (!all_aligned16(table, ids, out)) return misaligned();
+  if (is_one_of(out, table, ids)) return overlap();
   const hipError_t e = dlvm::launch_embedding_forward(dtype, vocab, width, tokens, table, ids, scale,
                                                       out, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? DLVM_OK : hip_fail(e, "embedding launch");
@@ -103,6 +109,7 @@ dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width,
   if (ws == nullptr || ws_bytes < dlvm::embedding_backward_ws(vocab, width, tokens))
     return fail(DLVM_ERR_WORKSPACE, "workspace missing or too small");
   if (!all_aligned16(ids, dout, dtable, ws)) return misaligned();
+  if (is_one_of(dtable, ids, dout)) return overlap();
   const hipError_t e = dlvm::launch_embedding_backward(dtype, vocab, width, tokens, ids, dout, scale,
                                                        accumulate != 0, dtable, ws,
                                                        static_cast<hipStream_t>(stream));
@@ -128,6 +135,7 @@ dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, 
   if (ws != nullptr && ws_bytes < dlvm::gated_scan_ws(dtype, steps, batch, width))
     return fail(DLVM_ERR_WORKSPACE, "workspace is smaller than dlvm_gated_scan_ws_bytes");
   if (!all_aligned16(z, x, h0, lens, hs, hT, ws)) return misaligned();
+  if (is_one_of(hs, z, x)) return overlap();
   dlvm::GatedScan c{};
   c.dtype = dtype;
   c.coupled = mode == DLVM_SCAN_COUPLED;
@@ -157,6 +165,7 @@ dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps,
   if (ws != nullptr && ws_bytes < dlvm::gated_scan_ws(dtype, steps, batch, width))
     return fail(DLVM_ERR_WORKSPACE, "workspace is smaller than dlvm_gated_scan_ws_bytes");
   if (!all_aligned16(z, x, h0, lens, hs, dhs, dhT, dz, dx, dh0, ws)) return misaligned();
+  if (is_one_of(dz, z, x, hs, dhs) || is_one_of(dx, z, x, hs, dhs, dz)) return overlap();
   dlvm::GatedScan c{};
   c.dtype = dtype;
   c.coupled = mode == DLVM_SCAN_COUPLED;

@@ -8,9 +8,10 @@
 // maximum is known. The entropy is log s - w / s: all terms of w have one sign, so it
 // has no cancellation beyond its own size. Alternatives are collected in the same pass:
 // from the first tile of a row comes a bound that at least `top` logits reach (the
-// top-th largest of 64 maxima of disjoint parts of it, taken again after 2, 4, ... tiles), and
-// the few logits that reach it are kept in LDS, in lists of the waves that are cut back to the `top` best when full. So the
-// common logit costs one comparison for eight, and any order of logits is right.
+// top-th largest of 64 maxima of disjoint parts of it, taken again after 2, 4, ... tiles),
+// and the few logits that reach it are kept in LDS, in lists of the waves that are cut back
+// to the `top` best when full. So the common logit costs one comparison for eight, and any
+// order of logits is right.
 // A row is a wave's where it is short, else a workgroup's; with a workspace, a call of few
 // rows cuts them into parts, joined by a second launch.
 // bf16 logits are bound by both memory and arithmetic (about ten operations for two
@@ -565,6 +566,17 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
   if (k.dlogp != nullptr) {
     token = k.tokens[row];
     gl = token == -1 ? 0.0f : token < 0 || token >= k.classes ? NAN : k.dlogp[row];
+  }
+  if (token == -1 && ge == 0.0f) {  // no adjoint: a row of padding, whatever its logits hold
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t c = at + (u * NT + tid) * N;
+      if (c + N <= k.classes)
+        *reinterpret_cast<OutVec<TD, N>*>(d + c) = OutVec<TD, N>{};
+      else
+        for (int64_t i = c; i < k.classes; ++i) d[i] = store_cast<TD>(0.0f);
+    }
+    return;
   }
   const bool masked = lse == -INFINITY && gl == gl;
   // -scale p (gl + ge (log p + H)) = p (a + b max(log p, -1e4)); p is 0 where the maximum acts

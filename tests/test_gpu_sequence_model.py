@@ -233,3 +233,107 @@ def test_token_by_token():
         assert torch.equal(i.int(), ids)
         assert_close(to_np(tlp), v.cpu().numpy(), 1e-5)
     assert_close(to_np(state), to_np(net.o["hT"]), TOL["f32"])
+
+
+class Calls:
+    """Calls that are cut: many steps of few states, more tokens than one workgroup sorts,
+    few rows of many classes; each with a workspace of its own."""
+
+    def __init__(self, dtype, seed):
+        import torch
+        r = np.random.default_rng([810, seed])
+        T, B, H, N, V, E, R, C = 2100, 3, 72, 20000, 3000, 72, 4, 60000
+        self.sizes, self.dtype = (T, B, H, N, V, E, R, C), dtype
+        st = torch_dtype(dtype)
+        host = lambda *s: r.standard_normal(s).astype(np.float32)  # noqa: E731
+        ids = np.where(r.random(N) < 0.3, 7, r.integers(-1, V, N)).astype(np.int32)
+        self.i = {k: to_dev(host(T, B, H), dtype) for k in ("z", "x", "dhs")}
+        self.i |= dict(h0=to_dev(host(B, H)), table=to_dev(host(V, E), dtype), de=to_dev(host(N, E), dtype),
+                       logits=to_dev(host(R, C), dtype), dlogp=to_dev(host(R)),
+                       ids=torch.from_numpy(ids).to(device()),
+                       tok=torch.from_numpy(r.integers(0, C, R).astype(np.int32)).to(device()))
+        new = lambda *s, dt=torch.float32: torch.full(s, float("nan"), dtype=dt, device=device())  # noqa: E731
+        self.o = {k: new(T, B, H, dt=st) for k in ("hs", "dz", "dx")}
+        self.o |= dict(hT=new(B, H), dh0=new(B, H), e=new(N, E, dt=st), dtable=new(V, E), logp=new(R), lse=new(R),
+                       ent=new(R), top_logp=new(R, 20), dlogits=new(R, C, dt=st))
+        self.top = torch.zeros((R, 20), dtype=torch.int32, device=device())
+        self.ws = [torch.full((n,), 255, dtype=torch.uint8, device=device())
+                   for n in (dl.gated_scan_ws_bytes(dtype, T, B, H), dl.embedding_backward_ws_bytes(V, E, N),
+                             dl.token_logprobs_ws_bytes(R, C, 20))]
+
+    def step(self, stream=None):
+        T, B, H, N, V, E, R, C = self.sizes
+        i, o, d = self.i, self.o, self.dtype
+        dl.gated_scan_forward(d, "coupled", T, B, H, i["z"], H, i["x"], H, i["h0"], None, o["hs"], H, o["hT"],
+                              self.ws[0], stream)
+        dl.gated_scan_backward(d, "coupled", T, B, H, i["z"], H, i["x"], H, i["h0"], None, o["hs"], H, i["dhs"], H,
+                               None, o["dz"], H, o["dx"], H, o["dh0"], self.ws[0], stream)
+        dl.embedding_forward(d, V, E, N, i["table"], i["ids"], 0.5, o["e"], stream)
+        dl.embedding_backward(d, V, E, N, i["ids"], i["de"], 0.5, False, o["dtable"], self.ws[1], stream)
+        dl.token_logprobs(d, R, C, i["logits"], C, 1.0, i["tok"], o["logp"], o["lse"], o["ent"], 20, self.top,
+                          o["top_logp"], self.ws[2], stream)
+        dl.token_logprobs_backward(d, d, R, C, i["logits"], C, 1.0, i["tok"], o["lse"], o["ent"], i["dlogp"], None,
+                                   o["dlogits"], C, stream)
+
+    def results(self):
+        import torch
+        torch.cuda.synchronize()
+        out = {k: v.clone() for k, v in self.o.items()} | {"top": self.top.clone()}
+        for v in self.o.values():
+            v.fill_(float("nan"))
+        self.top.fill_(-9)
+        torch.cuda.synchronize()
+        return out
+
+
+def _same_bits(got, want, what):
+    import torch
+    for k, v in got.items():
+        assert torch.equal(v, want[k]), (what, k)
+
+
+def test_calls_that_are_cut_captured_and_replayed():
+    """Two graphs with workspaces of their own, replayed with eager calls between and both
+    at once, give the eager calls' bits."""
+    import torch
+    calls = [Calls("bf16", 1), Calls("f32", 2)]
+    want = []
+    for c in calls:
+        c.step()
+        want.append(c.results())
+        assert all(not v.isnan().any() for v in want[-1].values())
+    graphs = []
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            c.step()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for turn in range(4):
+        for c, g, w in zip(calls, graphs, want):
+            for ws in c.ws:
+                ws.fill_(turn)
+            g.replay()
+            _same_bits(c.results(), w, turn)
+            c.step()
+            _same_bits(c.results(), w, turn)
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        for c, w in zip(calls, want):
+            _same_bits(c.results(), w, turn)
+
+
+def test_calls_that_are_cut_on_two_streams():
+    import torch
+    calls = [Calls("bf16", 3), Calls("f32", 4), Calls("f32", 5)]
+    want = []
+    for c in calls:
+        c.step()
+        want.append(c.results())
+    streams = [torch.cuda.Stream() for _ in calls]
+    for turn in range(4):
+        for c, s in zip(calls, streams):
+            c.step(s)
+        for c, w in zip(calls, want):
+            _same_bits(c.results(), w, turn)

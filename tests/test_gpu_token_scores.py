@@ -261,3 +261,29 @@ def test_cross_entropy_is_the_mean_of_minus_logp():
     assert abs(loss.item() + got["logp"].mean()) <= 8 * t * abs(loss.item()) + 8 * t
     g = _grad(zd, R, V, V, "f32", "f32", 1.0, tk, lse, ent, np.full(R, -1.0 / R, np.float32), None)
     assert np.abs(g - to_np(d)).max() <= 8 * t / R
+
+
+@pytest.mark.parametrize("types", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("V", [5, 1001, 9000])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradient_of_padding_is_zero(types, V, entropy):
+    """Rows of padding hold anything; with an adjoint of the entropy they are not padding."""
+    dtype, out = types
+    R = 6
+    r = _rng(9, V)
+    z = _logits(r, R, V, "plain")
+    tokens = np.array([0, -1, V - 1, -1, -1, 2], np.int32)
+    z[1], z[3, 0], z[4] = np.nan, np.inf, 1e30
+    dlogp = r.standard_normal(R).astype(np.float32)
+    dent = np.zeros(R, np.float32) if entropy else None
+    if entropy:
+        dent[3], dent[5] = 0.5, -2.0
+    _, (zd, tk, lse, ent) = _run(z, dtype, tokens, 1.0, 0)
+    got = _grad(zd, R, V, V, dtype, out, 1.0, tk, lse, ent, dlogp, dent)
+    assert (got[[1, 4]] == 0).all()
+    assert np.isnan(got[3]).all() if entropy else (got[3] == 0).all()
+    keep = [0, 2, 5]
+    q = quant(z, dtype)[keep]
+    sub = lambda v: None if v is None else v[keep]  # noqa: E731
+    ref = oracle.token_scores_vjp(q, tokens[keep], 1.0, dlogp[keep], sub(dent))
+    _same(got[keep], ref, _grad_tol(q, tokens[keep], 1.0, dlogp[keep], sub(dent), out, ref), "dlogits")

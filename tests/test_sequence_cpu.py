@@ -100,6 +100,21 @@ def test_gated_scan_backward_refuses(changes, status):
     assert _call("dlvm_gated_scan_backward", SCANB, changes) == status
 
 
+B, C, D, E, F = (A + 4096 * i for i in range(1, 6))
+
+
+@pytest.mark.parametrize("call,args,changes", [
+    ("dlvm_embedding_forward", LOOKUP, dict(ids=B)),
+    ("dlvm_embedding_backward", GRAD, dict(ids=B)),
+    ("dlvm_gated_scan_forward", SCAN, dict(x=B)), ("dlvm_gated_scan_forward", SCAN, dict(z=B)),
+    ("dlvm_gated_scan_backward", SCANB, dict(z=B, x=C, hs=D, dhs=E, dx=E)),
+    ("dlvm_gated_scan_backward", SCANB, dict(z=B, x=C, hs=D, dhs=E, dx=F, dz=B)),
+    ("dlvm_gated_scan_backward", SCANB, dict(z=B, x=C, hs=D, dhs=E, dx=F, dz=F)),
+])
+def test_outputs_in_place_of_inputs_are_refused(call, args, changes):
+    assert _call(call, args, changes) == INV
+
+
 def test_gated_scan_workspace():
     for dtype in ("f32", "bf16"):
         for t, b, h in ((1, 1, 1), (100000, 1, 64), (77, 1000, 1000)):
