@@ -550,20 +550,32 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
 }
 
 // ---------------------------------------------------------------------------
-// Choice of the variant, for N states: alone where a thread to each state fills the GPU
-// (sixteen waves on a compute unit) or there are no steps to share; chained, or in segments,
-// where the tiles of states leave compute units idle for so many steps that it pays for
-// another launch and the waiting, or the second reading. Forward, bf16, in one piece against
-// chained: 8 tiles, T 1024 20.8 and 9.5 us, T 16384 295 and 21; 128 tiles, T 1024 22 and 16,
-// T 4096 76 and 44; 188 tiles, T 1024 24 and 27, T 2048 43 and 43. Gradient: 128 tiles, T 4096
-// 167 in one piece, 101 in four segments; 204 tiles of float32, T 777 56 and 50 in three.
+// Choice of the variant, for N states: alone where a thread to each state fills the GPU for
+// so few steps, chained, or in segments, where the tiles of states leave compute units idle
+// for so many steps that it pays for another launch and the waiting, or the second reading.
+// Forward and gradient in us, bf16, T steps of so many tiles of 64 states:
+//                          alone         shared
+//   1024 tiles, T 16    4.4 and 5.9    6.9 and 12.1
+//   512 tiles, T 32     5.8 and 8.3    5.0 and 7.7
+//   1024 tiles, T 32    6.4 and 9.6    7.4 and 12.5
+//   1024 tiles, T 64    9.1 and 15.9   8.4 and 12.8
+//   2048 tiles, T 64   15.1 and 23.9  13.4 and 23.6
+//   2048 tiles, T 128  26.8 and 45.4  23.1 and 40.1
+//   4096 tiles, T 64   23.0 and 35.8  24.7 and 45.4
+// Forward, bf16, in one piece against chained: 8 tiles, T 1024 20.8 and 9.5, T 16384 295 and
+// 21; 128 tiles, T 1024 22 and 16, T 4096 76 and 44; 188 tiles, T 1024 24 and 27, T 2048 43
+// and 43. Gradient in one piece against segments: 128 tiles, T 2048 80 and 54; 160 tiles,
+// T 777 36 and 31, T 300 16 and 18; 204 tiles, T 777 39 and 39, in float32 47 and 50.
 // ---------------------------------------------------------------------------
 constexpr int64_t kBlocks = 512;       // two workgroups on a compute unit
 constexpr int64_t kUncut = 192;        // tiles from which a gradient is not cut
 constexpr int64_t kUnchained = 160;    // and a forward call not chained
 constexpr int32_t kShortest = 128;     // steps of a segment at least
 
-bool alone(int64_t T, int64_t N) { return T <= 2 * kUnroll || (N + 63) / 64 >= 4096; }
+bool alone(int64_t T, int64_t N) {
+  const int64_t tiles = (N + 63) / 64;
+  return T <= 2 * kUnroll || tiles >= 4096 || T * 32 <= tiles;
+}
 bool chained(int64_t T, int64_t N) {
   return !alone(T, N) && (N + 63) / 64 < kUnchained && T >= 2 * kWaves * kChainedUnroll;
 }

@@ -12,8 +12,9 @@
 // and the few logits that reach it are kept in LDS, in lists of the waves that are cut back
 // to the `top` best when full. So the common logit costs one comparison for eight, and any
 // order of logits is right.
-// A row is a wave's where it is short, else a workgroup's; with a workspace, a call of few
-// rows cuts them into parts, joined by a second launch.
+// A row is a wave's where it is short or there are many, else a workgroup's of four or
+// eight; with a workspace, a call of few long rows cuts them into parts, joined by a second
+// launch.
 // bf16 logits are bound by both memory and arithmetic (about ten operations for two
 // bytes, the exponential four of them), float32 ones by memory.
 #include <math.h>
@@ -202,17 +203,17 @@ __device__ __forceinline__ float reached_by(float v, int top) {
   return key_logit(static_cast<uint64_t>(reached < lowest ? lowest : reached) << 32);
 }
 
-// Maximum over each eight lanes, in all of them.
-__device__ __forceinline__ float max_of_8(float v) {
-  v = fmaxf(v, row_rot<0xB1>(v));    // the other lane of a pair
-  v = fmaxf(v, row_rot<0x4E>(v));    // the other pair of four
-  return fmaxf(v, row_rot<0x141>(v));  // the other four
+// Maximum over each two, four or eight lanes, in all of them.
+template <int LANES> __device__ __forceinline__ float max_of(float v) {
+  static_assert(LANES == 2 || LANES == 4 || LANES == 8, "");
+  v = fmaxf(v, row_rot<0xB1>(v));                     // the other lane of a pair
+  if (LANES > 2) v = fmaxf(v, row_rot<0x4E>(v));      // the other pair of four
+  return LANES > 4 ? fmaxf(v, row_rot<0x141>(v)) : v;  // the other four
 }
 
 // ---------------------------------------------------------------------------
 // Scores. NW waves share a row (or a part of one); NW = 1: four rows to a workgroup.
 // ---------------------------------------------------------------------------
-constexpr int kRowWaves = 8;
 constexpr int kLogits = 16;  // of a thread in a tile (32 of bf16 took registers for waves: 233 against 218 us)
 constexpr int kUnroll = 4;   // vectors of a thread of the gradient in flight
 
@@ -375,10 +376,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
       // the next is written to the other)
       if ((done & (done - 1)) == 0) {
         float head = m;
-        if (NW > 1) {  // of eight threads, so that 64 heads cover the workgroup
+        if constexpr (NW > 1) {  // of NW threads, so that 64 heads cover the workgroup
           float* set = heads[__builtin_ctz(done) % 2];
-          head = max_of_8(m);
-          if (lane % 8 == 0) set[wave * 8 + lane / 8] = head;
+          head = max_of<NW>(m);
+          if (lane % NW == 0) set[(wave * 64 + lane) / NW] = head;
           __syncthreads();
           head = set[lane];
         }
@@ -620,18 +621,37 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
 // ---------------------------------------------------------------------------
 // Choice of the variant.
 // ---------------------------------------------------------------------------
+// us of scores with 5 alternatives, in rows x classes of bf16, by the waves to a row:
+//                   1      4      8
+//   256 x 1500     6.5           6.2
+//   1024 x 1500    6.6          10.8
+//   512 x 4000     9.8    6.4    7.2
+//   512 x 131072  89     36     32
+//   1024 x 4000   10.3    7.5   11.1
+//   1024 x 131072 94     54     55
+//   4096 x 4000   15.3   17.6   31.9
+//   4096 x 16000  33.7   37.5   52.6
+//   4096 x 32000  55.6   56.3   73.6
+// (A workgroup of more waves waits longer for the last of them at each of its barriers and
+// ranks more keys at the end; few rows want the waves.) And in parts, with the join, against
+// whole rows: 8 x 24000 10 and 8.8, 8 x 50000 10.4 and 11.6, 8 x 131072 10.9 and 19.3,
+// 96 x 50000 13.0 and 12.3, 96 x 131072 17.9 and 20.4 (and another launch).
 constexpr int64_t kWaveRow = 2048;      // classes up to which a wave takes a row
+constexpr int64_t kWaveRows = 4096;     // rows from which it takes one
+constexpr int64_t kWaveRowOfMany = 16384;  // of up to so many classes
+constexpr int64_t kFourRows = 768;      // rows from which four waves take one, else eight
+constexpr int64_t kCutRow = 65536;      // classes from which a row is cut into parts
+constexpr int64_t kCutRows = 128;       // where there are fewer rows
 constexpr int64_t kPartLen = 4096;      // classes of a part at least
 constexpr int64_t kBlocks = 512;        // workgroups that fill the GPU
 constexpr int64_t kTurn = 1 << 22;      // workgroups of a launch (its threads are counted in 32 bits)
 
 int parts_of(int64_t rows, int64_t classes, int64_t* len) {
   *len = classes;
-  if (classes <= kWaveRow || rows >= kBlocks / 2) return 1;
+  if (classes < kCutRow || rows >= kCutRows) return 1;
   int64_t S = kBlocks / rows;
   if (S > classes / kPartLen) S = classes / kPartLen;
   if (S > kMaxParts) S = kMaxParts;
-  if (S <= 1) return 1;
   const int64_t L = ((classes + S - 1) / S + 511) / 512 * 512;
   *len = L;
   return static_cast<int>((classes + L - 1) / L);
@@ -643,9 +663,9 @@ template <typename T> hipError_t scores(const TokenScores& c, void* ws, hipStrea
   if (cut.parts > 1) {
     cut.keys = static_cast<uint64_t*>(ws);
     cut.stats = reinterpret_cast<Part*>(cut.keys + c.rows * cut.parts * c.top);
-    launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, kRowWaves, true, true>
-                            : dlvm_token_scores_kernel<T, kRowWaves, false, true>,
-                  dim3(static_cast<uint32_t>(c.rows * cut.parts)), dim3(64 * kRowWaves), s, c, cut);
+    launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 8, true, true>
+                            : dlvm_token_scores_kernel<T, 8, false, true>,
+                  dim3(static_cast<uint32_t>(c.rows * cut.parts)), dim3(512), s, c, cut);
     launch_kernel(dlvm_token_scores_join_kernel<T>, dim3(static_cast<uint32_t>(c.rows)), dim3(256), s, c, cut);
     return hipGetLastError();
   }
@@ -661,14 +681,19 @@ template <typename T> hipError_t scores(const TokenScores& c, void* ws, hipStrea
       t.top_ids += r0 * c.top;
       t.top_logp += r0 * c.top;
     }
-    if (c.classes <= kWaveRow)
+    const uint32_t rows = static_cast<uint32_t>(t.rows);
+    if (c.classes <= kWaveRow || (c.rows >= kWaveRows && c.classes <= kWaveRowOfMany))
       launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 1, true, false>
                               : dlvm_token_scores_kernel<T, 1, false, false>,
-                    dim3(static_cast<uint32_t>((t.rows + 3) / 4)), dim3(256), s, t, cut);
+                    dim3((rows + 3) / 4), dim3(256), s, t, cut);
+    else if (c.rows >= kFourRows)
+      launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 4, true, false>
+                              : dlvm_token_scores_kernel<T, 4, false, false>,
+                    dim3(rows), dim3(256), s, t, cut);
     else
-      launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, kRowWaves, true, false>
-                              : dlvm_token_scores_kernel<T, kRowWaves, false, false>,
-                    dim3(static_cast<uint32_t>(t.rows)), dim3(64 * kRowWaves), s, t, cut);
+      launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 8, true, false>
+                              : dlvm_token_scores_kernel<T, 8, false, false>,
+                    dim3(rows), dim3(512), s, t, cut);
   }
   return hipGetLastError();
 }

@@ -242,7 +242,7 @@ class Calls:
     def __init__(self, dtype, seed):
         import torch
         r = np.random.default_rng([810, seed])
-        T, B, H, N, V, E, R, C = 2100, 3, 72, 20000, 3000, 72, 4, 60000
+        T, B, H, N, V, E, R, C = 2100, 3, 72, 20000, 3000, 72, 4, 70000
         self.sizes, self.dtype = (T, B, H, N, V, E, R, C), dtype
         st = torch_dtype(dtype)
         host = lambda *s: r.standard_normal(s).astype(np.float32)  # noqa: E731
