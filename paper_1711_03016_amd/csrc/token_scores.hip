@@ -632,6 +632,10 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
 //   4096 x 4000   15.3   17.6   31.9
 //   4096 x 16000  33.7   37.5   52.6
 //   4096 x 32000  55.6   56.3   73.6
+//   4096 x 65536         103    104
+//   4096 x 131072        194    185
+//   4096 x 8000 float32   31     32     41
+//   4096 x 32000 float32  94     96     93
 // (A workgroup of more waves waits longer for the last of them at each of its barriers and
 // ranks more keys at the end; few rows want the waves.) And in parts, with the join, against
 // whole rows: 8 x 24000 10 and 8.8, 8 x 50000 10.4 and 11.6, 8 x 131072 10.9 and 19.3,
@@ -639,7 +643,8 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
 constexpr int64_t kWaveRow = 2048;      // classes up to which a wave takes a row
 constexpr int64_t kWaveRows = 4096;     // rows from which it takes one
 constexpr int64_t kWaveRowOfMany = 16384;  // of up to so many classes
-constexpr int64_t kFourRows = 768;      // rows from which four waves take one, else eight
+constexpr int64_t kFourRows = 768;      // rows from which four waves take one, else eight,
+constexpr int64_t kFourBytes = 96 << 10;  // if it has up to so many bytes
 constexpr int64_t kCutRow = 65536;      // classes from which a row is cut into parts
 constexpr int64_t kCutRows = 128;       // where there are fewer rows
 constexpr int64_t kPartLen = 4096;      // classes of a part at least
@@ -686,7 +691,7 @@ template <typename T> hipError_t scores(const TokenScores& c, void* ws, hipStrea
       launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 1, true, false>
                               : dlvm_token_scores_kernel<T, 1, false, false>,
                     dim3((rows + 3) / 4), dim3(256), s, t, cut);
-    else if (c.rows >= kFourRows)
+    else if (c.rows >= kFourRows && c.classes * static_cast<int64_t>(sizeof(T)) <= kFourBytes)
       launch_kernel(c.top > 0 ? dlvm_token_scores_kernel<T, 4, true, false>
                               : dlvm_token_scores_kernel<T, 4, false, false>,
                     dim3(rows), dim3(256), s, t, cut);
