@@ -188,17 +188,20 @@ __device__ __forceinline__ void append_carefully(volatile uint64_t* list, Wanted
   }
 }
 
-// A logit that at least `top` of the wave's 64 values reach: the top-th largest with its last
-// 16 bits cleared, found bit by bit from counts of the values that reach a number. (One
-// comparison a bit: 64 values ranked against each other cost more than the rest of a tile.)
-__device__ __forceinline__ float reached_by(float v, int top) {
-  const uint32_t mine = static_cast<uint32_t>(rank_key(v, 0) >> 32);
+// A number that at least `top` of the wave's 64 reach: the top-th largest with its last 16
+// bits cleared, found bit by bit from counts of those that reach a number. (One comparison a
+// bit: 64 values ranked against each other cost more than the rest of a tile.)
+__device__ __forceinline__ uint32_t reached_by(uint32_t mine, int top) {
   uint32_t reached = 0;
 #pragma unroll
   for (int b = 31; b >= 16; --b) {
     const uint32_t with = reached | (1u << b);
     if (__builtin_popcountll(__ballot(mine >= with)) >= top) reached = with;
   }
+  return reached;
+}
+__device__ __forceinline__ float reached_by(float v, int top) {
+  const uint32_t reached = reached_by(static_cast<uint32_t>(rank_key(v, 0) >> 32), top);
   constexpr uint32_t lowest = 0x007fffffu;  // of -infinity
   return key_logit(static_cast<uint64_t>(reached < lowest ? lowest : reached) << 32);
 }
@@ -474,9 +477,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void dlvm_token_scores_ker
   }
 }
 
-// The parts of a row: their sums joined in order, and the best of their keys. At least
-// `top` keys reach the least of the parts' q-th logits, q parts' share of `top`, so those
-// below are not ranked. All loads are sent before the first is waited for.
+// The parts of a row: their sums joined in order, and the best of their keys. Those below what
+// `top` of the parts' first keys reach are not ranked (64 first keys or all, never fewer
+// than `top`). All loads are sent before the first is waited for.
 constexpr int kMaxParts = 64;
 constexpr int kJoinKeys = kMaxParts * kTopMax / 256;  // of a thread
 
@@ -487,14 +490,16 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x;
   const float c2 = k.scale * kLog2e;
-  const int share = (k.top + cut.parts - 1) / cut.parts, total = cut.parts * k.top;
+  const int total = cut.parts * k.top;
   const uint64_t* from = cut.keys + row * total;
   const int own = lane < cut.parts ? lane : 0;
   Part p = cut.stats[row * cut.parts + own];
   uint64_t mine[kJoinKeys] = {};
-  uint32_t least = 0xffffffffu;
+  uint32_t first = 0;
   if (k.top > 0) {
-    least = static_cast<uint32_t>(from[own * k.top + share - 1] >> 32);
+    const int j = lane / cut.parts;
+    const bool has = j < 64 / cut.parts && j < k.top;
+    first = has ? static_cast<uint32_t>(from[(lane - j * cut.parts) * k.top + j] >> 32) : 0;
 #pragma unroll
     for (int i = 0; i < kJoinKeys; ++i)
       if (256 * i < total) mine[i] = from[tid + 256 * i < total ? tid + 256 * i : total - 1];
@@ -510,11 +515,7 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores
   const bool masked = masked_everywhere(p, k.scale);
   if (tid == 0) write_scores(k, row, p, log_s, masked, zt);
   if (k.top == 0) return;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const uint32_t other = __shfl_xor(least, o, 64);
-    least = other < least ? other : least;
-  }
+  const uint32_t least = reached_by(first, k.top);
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kJoinKeys; ++i)
