@@ -638,23 +638,26 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
 //   4096 x 8000 float32   31     32     41
 //   4096 x 32000 float32  94     96     93
 // (A workgroup of more waves waits longer for the last of them at each of its barriers and
-// ranks more keys at the end; few rows want the waves.) And in parts, with the join, against
-// whole rows: 8 x 24000 10 and 8.8, 8 x 50000 10.4 and 11.6, 8 x 131072 10.9 and 19.3,
-// 96 x 50000 13.0 and 12.3, 96 x 131072 17.9 and 20.4 (and another launch).
+// ranks more keys at the end; few rows want the waves.) Whole rows against parts and their
+// join, of both launches with what lies between: with 20 alternatives 8 x 32000 12.9 and
+// 11.4, 8 x 50000 14.9 and 11.2, with 5 1 x 32000 9.4 and 10.3, 32 x 32000 10.3 and 10.2,
+// 96 x 50000 12.2 and 12.6; with none 1 x 50000 6.9 and 8.9, 1 x 100000 10.8 and 10.5,
+// 8 x 131072 13.1 and 11.1.
 constexpr int64_t kWaveRow = 2048;      // classes up to which a wave takes a row
 constexpr int64_t kWaveRows = 4096;     // rows from which it takes one
 constexpr int64_t kWaveRowOfMany = 16384;  // of up to so many classes
 constexpr int64_t kFourRows = 768;      // rows from which four waves take one, else eight,
 constexpr int64_t kFourBytes = 96 << 10;  // if it has up to so many bytes
-constexpr int64_t kCutRow = 65536;      // classes from which a row is cut into parts
+constexpr int64_t kCutRow = 32768;      // classes from which a row is cut into parts,
+constexpr int64_t kCutPlain = 98304;    // or these without alternatives,
 constexpr int64_t kCutRows = 128;       // where there are fewer rows
 constexpr int64_t kPartLen = 4096;      // classes of a part at least
 constexpr int64_t kBlocks = 512;        // workgroups that fill the GPU
 constexpr int64_t kTurn = 1 << 22;      // workgroups of a launch (its threads are counted in 32 bits)
 
-int parts_of(int64_t rows, int64_t classes, int64_t* len) {
+int parts_of(int64_t rows, int64_t classes, int top, int64_t* len) {
   *len = classes;
-  if (classes < kCutRow || rows >= kCutRows) return 1;
+  if (classes < (top > 0 ? kCutRow : kCutPlain) || rows >= kCutRows) return 1;
   int64_t S = kBlocks / rows;
   if (S > classes / kPartLen) S = classes / kPartLen;
   if (S > kMaxParts) S = kMaxParts;
@@ -665,7 +668,7 @@ int parts_of(int64_t rows, int64_t classes, int64_t* len) {
 
 template <typename T> hipError_t scores(const TokenScores& c, void* ws, hipStream_t s) {
   Cut cut{1, c.classes, nullptr, nullptr};
-  if (ws != nullptr) cut.parts = parts_of(c.rows, c.classes, &cut.len);
+  if (ws != nullptr) cut.parts = parts_of(c.rows, c.classes, c.top, &cut.len);
   if (cut.parts > 1) {
     cut.keys = static_cast<uint64_t*>(ws);
     cut.stats = reinterpret_cast<Part*>(cut.keys + c.rows * cut.parts * c.top);
@@ -731,7 +734,7 @@ template <typename T, typename TD> hipError_t grad(ScoresGrad g, hipStream_t s) 
 
 size_t token_scores_ws(int64_t rows, int64_t classes, int top) {
   int64_t len = 0;
-  const int64_t parts = parts_of(rows, classes, &len);
+  const int64_t parts = parts_of(rows, classes, top, &len);
   return parts == 1 ? 256 : static_cast<size_t>(rows * parts) * (top * 8 + sizeof(Part));
 }
 
