@@ -465,64 +465,103 @@ def sgd(dtype, n, params, master, grads, lr, stream=None):
 # ---------------------------------------------------------------------------
 # sequence operators: token embeddings, gated linear recurrence, token scores
 # ---------------------------------------------------------------------------
-_TORCH = None  # (torch, types by name, current stream's address by device)
+_TORCH = None  # (torch, types by name, current device, current stream's address by device)
 
 
 def _torch():
-    """torch, its types of the storage names, of ids and of workspaces, and what gives the
-    address of the current stream (a stream object made for its address costs half of
-    what a launch does)."""
+    """torch, its types by the names that ``_Call`` has for them, and what gives the current
+    device and the address of its current stream (a stream object made for its address
+    costs half of what a launch does)."""
     global _TORCH
     if _TORCH is None:
         import torch
         types = {"f32": torch.float32, "bf16": torch.bfloat16, "i32": torch.int32,
                  "ws": torch.uint8}
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream",
                       lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-        _TORCH = torch, types, raw
+        _TORCH = torch, types, device, raw
     return _TORCH
 
 
-def _call(fn, stream, tensors, *args):
-    """`fn(*args, stream)` on the GPU of `tensors`, ((name, tensor or None or address,
-    type name), ...): tensors of another type, on the host or on a second GPU are refused,
-    sizes and strides are the caller's, as in C."""
-    torch, types, raw = _TORCH or _torch()
-    dev = None
-    for name, t, ty in tensors:
-        if t is None or t.__class__ is int:
-            continue
-        if t.dtype is not types[ty]:
-            raise DlvmError(ERR_INVALID_ARG, f"{name} is {t.dtype}, not {types[ty]}")
-        d = t.get_device()
-        if d != dev:
-            if d < 0:
-                raise DlvmError(ERR_INVALID_ARG, f"{name} is not in GPU memory")
-            if dev is not None:
-                raise DlvmError(ERR_INVALID_ARG, f"{name} is on GPU {d}, another tensor on {dev}")
-            dev = d
-    if dev is None:
-        status = fn(*args, _stream(stream))
-    elif dev == torch.cuda.current_device():
-        status = fn(*args, raw(dev) if stream is None else _stream(stream))
-    else:
-        if stream is not None and stream.__class__ is not int and stream.device.index != dev:
-            raise DlvmError(ERR_INVALID_ARG, f"the stream is not on GPU {dev}")
-        with torch.cuda.device(dev):
-            status = fn(*args, raw(dev) if stream is None else _stream(stream))
-    if status != OK:
-        _check(status)
+class _Call:
+    """An entry point with the tensors it takes, "name" or "name:type" each (the storage type
+    if none is given; "out" for that of an output). Tensors of another type, on the host or
+    on a second GPU are refused; sizes and strides are the caller's, as in C."""
+
+    def __init__(self, function, tensors):
+        self.function = function
+        self.tensors = [t.split(":") for t in tensors.split()]
+        self.fn = None
+        self.types = {}
+
+    def _types(self, key):
+        if _TORCH is None:
+            _torch()
+        self.fn = getattr(lib(), self.function)
+        dtype, out = key if key.__class__ is tuple else (key, key)
+        names = {"out": out} | {k: k for k in _TORCH[1]}
+        self.types[key] = tuple(_TORCH[1][names[t[1]] if len(t) > 1 else dtype] for t in self.tensors)
+        return self.types[key]
+
+    def _refuse(self, i, what):
+        raise DlvmError(ERR_INVALID_ARG, f"{self.tensors[i][0]} is {what}")
+
+    def addresses(self, key, tensors):
+        """The GPU of `tensors` (each may be None or an address) and their addresses; `key` is
+        the storage type's name, or its and the output's."""
+        dev, at = None, []
+        for t, ty in zip(tensors, self.types.get(key) or self._types(key)):
+            if t is None or t.__class__ is int:
+                at.append(t)
+                continue
+            if t.dtype is not ty:
+                self._refuse(len(at), f"{t.dtype}, not {ty}")
+            d = t.get_device()
+            if d != dev:
+                if d < 0:
+                    self._refuse(len(at), "not in GPU memory")
+                if dev is not None:
+                    self._refuse(len(at), f"on GPU {d}, another tensor on {dev}")
+                dev = d
+            at.append(t.data_ptr())
+        return dev, at
+
+    def __call__(self, dev, stream, *args):
+        """The call with `args` on GPU `dev` (None: the current one)."""
+        torch, _, device, raw = _TORCH
+        if stream is not None and stream.__class__ is not int:
+            if dev is not None and stream.device.index != dev:
+                raise DlvmError(ERR_INVALID_ARG, f"the stream is not on GPU {dev}")
+            stream = stream.cuda_stream
+        if dev is None or dev == device():
+            status = self.fn(*args, raw(device()) if stream is None else stream)
+        else:
+            with torch.cuda.device(dev):
+                status = self.fn(*args, raw(dev) if stream is None else stream)
+        if status != OK:
+            _check(status)
 
 
-def _ws_args(ws):
-    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+_EMBED = _Call("dlvm_embedding_forward", "table ids:i32 out")
+_EMBED_BACK = _Call("dlvm_embedding_backward", "ids:i32 dout dtable:f32 ws:ws")
+_SCAN = _Call("dlvm_gated_scan_forward", "z x h0:f32 lens:i32 hs hT:f32 ws:ws")
+_SCAN_BACK = _Call("dlvm_gated_scan_backward",
+                   "z x h0:f32 lens:i32 hs dhs dhT:f32 dz dx dh0:f32 ws:ws")
+_SCORES = _Call("dlvm_token_logprobs",
+                "logits tokens:i32 logp:f32 lse:f32 entropy:f32 top_ids:i32 top_logp:f32 ws:ws")
+_SCORES_BACK = _Call("dlvm_token_logprobs_backward",
+                     "logits tokens:i32 lse:f32 entropy:f32 dlogp:f32 dentropy:f32 dlogits:out")
+
+
+def _bytes(ws):
+    return 0 if ws is None else ws.numel()
 
 
 def embedding_forward(dtype, vocab, width, tokens, table, ids, scale, out, stream=None):
     """out[i] = scale * table[ids[i]] (``dlvm_embedding_forward``)."""
-    _call(lib().dlvm_embedding_forward, stream,
-          (("table", table, dtype), ("ids", ids, "i32"), ("out", out, dtype)),
-          DTYPES[dtype], vocab, width, tokens, _ptr(table), _ptr(ids), float(scale), _ptr(out))
+    dev, (table, ids, out) = _EMBED.addresses(dtype, (table, ids, out))
+    _EMBED(dev, stream, DTYPES[dtype], vocab, width, tokens, table, ids, float(scale), out)
 
 
 def embedding_backward_ws_bytes(vocab: int, width: int, tokens: int) -> int:
@@ -532,11 +571,10 @@ def embedding_backward_ws_bytes(vocab: int, width: int, tokens: int) -> int:
 def embedding_backward(dtype, vocab, width, tokens, ids, dout, scale, accumulate, dtable, ws,
                        stream=None):
     """dtable[v] (+)= scale * the sum of dout[i] over ids[i] == v (``dlvm_embedding_backward``)."""
-    p, n = _ws_args(ws)
-    _call(lib().dlvm_embedding_backward, stream,
-          (("ids", ids, "i32"), ("dout", dout, dtype), ("dtable", dtable, "f32"), ("ws", ws, "ws")),
-          DTYPES[dtype], vocab, width, tokens, _ptr(ids), _ptr(dout), float(scale),
-          int(bool(accumulate)), _ptr(dtable), p, n)
+    size = _bytes(ws)
+    dev, (ids, dout, dtable, ws) = _EMBED_BACK.addresses(dtype, (ids, dout, dtable, ws))
+    _EMBED_BACK(dev, stream, DTYPES[dtype], vocab, width, tokens, ids, dout, float(scale),
+                1 if accumulate else 0, dtable, ws, size)
 
 
 def gated_scan_ws_bytes(dtype, steps: int, batch: int, width: int) -> int:
@@ -547,26 +585,21 @@ def gated_scan_forward(dtype, mode, steps, batch, width, z, ldz, x, ldx, h0, len
                        ws=None, stream=None):
     """h_t = a_t h_{t-1} + x_t ("free") or + (1 - a_t) x_t ("coupled"), a = sigmoid(z)
     (``dlvm_gated_scan_forward``); h0, lens, hT and ws may be None."""
-    p, n = _ws_args(ws)
-    _call(lib().dlvm_gated_scan_forward, stream,
-          (("z", z, dtype), ("x", x, dtype), ("h0", h0, "f32"), ("lens", lens, "i32"),
-           ("hs", hs, dtype), ("hT", hT, "f32"), ("ws", ws, "ws")),
-          DTYPES[dtype], SCAN_MODES[mode], steps, batch, width, _ptr(z), ldz, _ptr(x), ldx,
-          _ptr(h0), _ptr(lens), _ptr(hs), ldh, _ptr(hT), p, n)
+    size = _bytes(ws)
+    dev, (z, x, h0, lens, hs, hT, ws) = _SCAN.addresses(dtype, (z, x, h0, lens, hs, hT, ws))
+    _SCAN(dev, stream, DTYPES[dtype], SCAN_MODES[mode], steps, batch, width, z, ldz, x, ldx, h0,
+          lens, hs, ldh, hT, ws, size)
 
 
 def gated_scan_backward(dtype, mode, steps, batch, width, z, ldz, x, ldx, h0, lens, hs, ldh, dhs,
                         lddh, dhT, dz, lddz, dx, lddx, dh0, ws=None, stream=None):
     """Gradient of the recurrence for the adjoints dhs of hs and dhT of the last state
     (``dlvm_gated_scan_backward``); h0, lens, one of dhs and dhT, dh0 and ws may be None."""
-    p, n = _ws_args(ws)
-    _call(lib().dlvm_gated_scan_backward, stream,
-          (("z", z, dtype), ("x", x, dtype), ("h0", h0, "f32"), ("lens", lens, "i32"),
-           ("hs", hs, dtype), ("dhs", dhs, dtype), ("dhT", dhT, "f32"), ("dz", dz, dtype),
-           ("dx", dx, dtype), ("dh0", dh0, "f32"), ("ws", ws, "ws")),
-          DTYPES[dtype], SCAN_MODES[mode], steps, batch, width, _ptr(z), ldz, _ptr(x), ldx,
-          _ptr(h0), _ptr(lens), _ptr(hs), ldh, _ptr(dhs), lddh, _ptr(dhT), _ptr(dz), lddz,
-          _ptr(dx), lddx, _ptr(dh0), p, n)
+    size = _bytes(ws)
+    dev, (z, x, h0, lens, hs, dhs, dhT, dz, dx, dh0, ws) = _SCAN_BACK.addresses(
+        dtype, (z, x, h0, lens, hs, dhs, dhT, dz, dx, dh0, ws))
+    _SCAN_BACK(dev, stream, DTYPES[dtype], SCAN_MODES[mode], steps, batch, width, z, ldz, x, ldx,
+               h0, lens, hs, ldh, dhs, lddh, dhT, dz, lddz, dx, lddx, dh0, ws, size)
 
 
 def token_logprobs_ws_bytes(rows: int, classes: int, top: int) -> int:
@@ -577,25 +610,21 @@ def token_logprobs(dtype, rows, classes, logits, ld, scale, tokens, logp, lse, e
                    top_ids, top_logp, ws=None, stream=None):
     """Log probabilities of tokens, log-sum-exp, entropy and the `top` largest alternatives
     of each row (``dlvm_token_logprobs``); outputs not wanted are None."""
-    p, n = _ws_args(ws)
-    _call(lib().dlvm_token_logprobs, stream,
-          (("logits", logits, dtype), ("tokens", tokens, "i32"), ("logp", logp, "f32"),
-           ("lse", lse, "f32"), ("entropy", entropy, "f32"), ("top_ids", top_ids, "i32"),
-           ("top_logp", top_logp, "f32"), ("ws", ws, "ws")),
-          DTYPES[dtype], rows, classes, _ptr(logits), ld, float(scale), _ptr(tokens), _ptr(logp),
-          _ptr(lse), _ptr(entropy), top, _ptr(top_ids), _ptr(top_logp), p, n)
+    size = _bytes(ws)
+    dev, (logits, tokens, logp, lse, entropy, top_ids, top_logp, ws) = _SCORES.addresses(
+        dtype, (logits, tokens, logp, lse, entropy, top_ids, top_logp, ws))
+    _SCORES(dev, stream, DTYPES[dtype], rows, classes, logits, ld, float(scale), tokens, logp,
+            lse, entropy, top, top_ids, top_logp, ws, size)
 
 
 def token_logprobs_backward(dtype, out_dtype, rows, classes, logits, ld, scale, tokens, lse,
                             entropy, dlogp, dentropy, dlogits, ld_out, stream=None):
     """Gradient of logp and entropy with respect to the logits
     (``dlvm_token_logprobs_backward``); dlogp or dentropy may be None."""
-    _call(lib().dlvm_token_logprobs_backward, stream,
-          (("logits", logits, dtype), ("tokens", tokens, "i32"), ("lse", lse, "f32"),
-           ("entropy", entropy, "f32"), ("dlogp", dlogp, "f32"), ("dentropy", dentropy, "f32"),
-           ("dlogits", dlogits, out_dtype)),
-          DTYPES[dtype], DTYPES[out_dtype], rows, classes, _ptr(logits), ld, float(scale),
-          _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), ld_out)
+    dev, (logits, tokens, lse, entropy, dlogp, dentropy, dlogits) = _SCORES_BACK.addresses(
+        (dtype, out_dtype), (logits, tokens, lse, entropy, dlogp, dentropy, dlogits))
+    _SCORES_BACK(dev, stream, DTYPES[dtype], DTYPES[out_dtype], rows, classes, logits, ld,
+                 float(scale), tokens, lse, entropy, dlogp, dentropy, dlogits, ld_out)
 
 
 # ---------------------------------------------------------------------------
