@@ -214,6 +214,7 @@ __device__ __forceinline__ int32_t wave_max(int32_t v) {
   }
   return __builtin_amdgcn_readfirstlane(v);
 }
+__device__ __forceinline__ int32_t wave_min(int32_t v) { return -wave_max(-v); }
 
 // The tile of a workgroup, of n: workgroups go to the eight XCDs in turn, and neighbouring
 // tiles to one of them, since the rows of an odd width begin and end inside cache lines,
@@ -267,11 +268,15 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
 
   float h = k.h0 != nullptr && block == 0 ? k.h0[p.j] : 0.0f;
   E z[U] = {}, x[U] = {};
+  // Steps below `sure` are live in every lane, those from `over` on in none (the waves of a
+  // workgroup have the same states, so the same bounds).
+  const int32_t sure = k.lens == nullptr ? end : wave_min(p.on ? live : end);
+  const int32_t over = MODE == CHAINED || k.lens == nullptr ? end : wave_max(live);
   // Loads without conditions, steps behind the last that is live in any lane from that
   // one: in a branch of its own each load would be waited for before the next is sent.
   const int32_t stop = (k.lens == nullptr ? end : wave_max(live > begin ? live : begin + 1)) - 1;
   const auto fetch = [&](int32_t t0) {
-    if (t0 >= end) return;
+    if (t0 >= over) return;
     const int32_t from = t0 < stop ? t0 : stop;
     auto rz = pz.row(from), rx = px.row(from);
 #pragma unroll
@@ -287,7 +292,8 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   asm volatile("" : "+v"(h));  // every wave has its first state before one can write hT over it
 
   int phase = 0;
-  for (int32_t t0 = begin; t0 < end; t0 += NW * U) {
+  int32_t t0 = begin;
+  for (; t0 < over; t0 += NW * U) {
     const int32_t t = t0 + w * U;
     float a[U], q[U];
 #pragma unroll
@@ -297,7 +303,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
       const float xv = load_as_f32(&x[u]);
       q[u] = COUPLED ? c * xv : xv;
     }
-    const bool whole = k.lens == nullptr && t + U <= end;  // every step of the thread is live
+    const bool whole = t + U <= sure;
     if (!whole)
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -355,6 +361,8 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
     if (MODE == ALONE) h = now;
     if (MODE == CHAINED) break;  // a block is one round
   }
+  if (MODE != CHAINED && p.on)
+    for (int32_t t = t0 + w; t < end; t += NW) ph.in(ph.row(t)) = store_cast<E>(0.0f);
   if (k.hT != nullptr && p.on && w == 0 && end == T) k.hT[p.j] = h;
 }
 
@@ -377,7 +385,6 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;
   const int32_t end = T - begin < cut.len ? T : begin + cut.len;
-  const int32_t last = begin + (end - begin - 1) / (NW * U) * (NW * U);  // first step of the last block
   const int32_t n = length_of(k.lens, p.b, k.T);
   const int32_t live = !p.on ? 0 : n < end ? n : end;
   const bool has_d = k.dhs != nullptr;
@@ -388,8 +395,13 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   const float* first = cut.S > 1 ? cut.init : k.dhT;
   float mu = first != nullptr ? first[p.j] : 0.0f;
   E z[U] = {}, x[U] = {}, d[U] = {}, before = {};
+  // as in the forward call
+  const int32_t sure = k.lens == nullptr ? end : wave_min(p.on ? live : end);
+  const int32_t over = k.lens == nullptr ? end : wave_max(live);
+  const int32_t rounds = over > begin ? (over - begin + NW * U - 1) / (NW * U) : 0;
+  const int32_t last = begin + (rounds - 1) * (NW * U);  // first step of the last round
   const int32_t stop = (k.lens == nullptr ? end : wave_max(live > begin ? live : begin + 1)) - 1;
-  const auto fetch = [&](int32_t t0) {  // as in the forward call
+  const auto fetch = [&](int32_t t0) {
     if (t0 < begin) return;
     const int32_t from = t0 < stop ? t0 : stop;
     auto rz = pz.row(from), rx = px.row(from), rd = pd.row(from);
@@ -412,6 +424,11 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
     mu = fmaf(m.x, mu, m.y);
   }
 
+  if (p.on)
+    for (int32_t t = last + NW * U + w; t < end; t += NW) {
+      gz.in(gz.row(t)) = store_cast<E>(0.0f);
+      gx.in(gx.row(t)) = store_cast<E>(0.0f);
+    }
   int phase = 0;
   for (int32_t t0 = last; t0 >= begin; t0 -= NW * U) {
     const int32_t t = t0 + w * U;
@@ -425,7 +442,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
       f[u] = (COUPLED ? prev - xv : prev) * c[u];
       prev = a[u] * prev + (COUPLED ? c[u] * xv : xv);
     }
-    const bool whole = k.lens == nullptr && has_d && t + U <= end;  // every step is live
+    const bool whole = has_d && t + U <= sure;
     if (!whole)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
