@@ -582,10 +582,14 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
 // Forward, bf16, in one piece against chained: 8 tiles, T 1024 20.8 and 9.5, T 16384 295 and
 // 21; 128 tiles, T 1024 22 and 16, T 4096 76 and 44; 188 tiles, T 1024 24 and 27, T 2048 43
 // and 43. Gradient in one piece against segments: 128 tiles, T 2048 80 and 54; 160 tiles,
-// T 777 36 and 31, T 300 16 and 18; 204 tiles, T 777 39 and 39, in float32 47 and 50.
+// T 777 36 and 31, T 300 16 and 18; 204 tiles, T 777 39 and 39, in float32 47 and 50. Where
+// sequences end at lengths the longest hold a few compute units longest: 204 tiles, T 777,
+// float32 50 and 46; 192 tiles, T 2048 87 and 70; 320 tiles, T 2048 132 and 114; 384 tiles,
+// T 1024, float32 92 and 102.
 // ---------------------------------------------------------------------------
 constexpr int64_t kBlocks = 512;       // two workgroups on a compute unit
 constexpr int64_t kUncut = 192;        // tiles from which a gradient is not cut
+constexpr int64_t kUncutRagged = 352;  // where sequences have lengths
 constexpr int64_t kUnchained = 160;    // and a forward call not chained
 constexpr int32_t kShortest = 128;     // steps of a segment at least
 
@@ -598,9 +602,9 @@ bool chained(int64_t T, int64_t N) {
 }
 
 // Segments of a gradient, and the steps of one.
-int segments(int64_t T, int64_t N, int32_t* len) {
+int segments(int64_t T, int64_t N, bool ragged, int32_t* len) {
   const int64_t tiles = (N + 63) / 64, step = kWaves * kUnroll;
-  int64_t S = alone(T, N) || tiles >= kUncut ? 1 : (kBlocks + tiles - 1) / tiles;
+  int64_t S = alone(T, N) || tiles >= (ragged ? kUncutRagged : kUncut) ? 1 : (kBlocks + tiles - 1) / tiles;
   if (S > T / kShortest) S = T / kShortest;
   if (S < 1) S = 1;
   const int64_t L = S == 1 ? T : ((T + S - 1) / S + step - 1) / step * step;
@@ -642,7 +646,7 @@ template <typename E, bool COUPLED> hipError_t backward(const GatedScan& c, void
     return hipGetLastError();
   }
   const dim3 block(64 * kWaves);
-  if (ws != nullptr) cut.S = segments(c.T, N, &cut.len);
+  if (ws != nullptr) cut.S = segments(c.T, N, c.lens != nullptr, &cut.len);
   if (cut.S > 1) {
     cut.init = static_cast<float*>(ws);
     cut.sums = reinterpret_cast<float2*>(cut.init + (N + 63) / 64 * 64);
@@ -656,7 +660,7 @@ template <typename E, bool COUPLED> hipError_t backward(const GatedScan& c, void
 
 size_t gated_scan_ws(int, int64_t T, int64_t B, int64_t H) {
   int32_t len = 0;
-  const int64_t N = B * H, S = segments(T, N, &len);
+  const int64_t N = B * H, S = segments(T, N, true, &len);  // as many as without lengths, or more
   const size_t tiles = static_cast<size_t>((N + 63) / 64);
   size_t bytes = S == 1 ? 256 : tiles * 64 * 4 + static_cast<size_t>(S) * N * 8;
   if (chained(T, N)) {
