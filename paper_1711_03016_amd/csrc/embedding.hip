@@ -98,7 +98,6 @@ constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = kDigits;                // one thread to a digit
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortBlock = 4 * kSortThreads;         // tokens of a block
 constexpr int kSmallSort = 8 * kSortThreads;
 constexpr int64_t kSortTokens = int64_t(1) << 18;    // tokens of one sort
 
@@ -178,6 +177,8 @@ struct SortIn {
   const int32_t* tok;
 };
 
+// W tokens of a block to each thread.
+template <int W>
 __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_count_kernel(int32_t V, int32_t N, int shift,
                                                                             int bits, SortIn in,
                                                                             int32_t* __restrict__ counts) {
@@ -185,8 +186,8 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_count_kernel(int3
   hist[threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < kSortBlock / kSortThreads; ++u) {
-    const int32_t i = blockIdx.x * kSortBlock + u * kSortThreads + threadIdx.x;
+  for (int u = 0; u < W; ++u) {
+    const int32_t i = (blockIdx.x * W + u) * kSortThreads + threadIdx.x;
     if (i < N) {
       const int32_t row = in.ids != nullptr ? row_of(in.ids[i], V) : in.row[i];
       atomicAdd(&hist[(row >> shift) & ((1 << bits) - 1)], 1);
@@ -196,10 +197,11 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_count_kernel(int3
   counts[blockIdx.x * kDigits + threadIdx.x] = hist[threadIdx.x];
 }
 
+template <int W>
 __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
     int32_t V, int32_t N, int shift, int bits, SortIn in, const int32_t* __restrict__ counts,
     int32_t* __restrict__ row_out, int32_t* __restrict__ tok_out) {
-  constexpr int W = kSortBlock / kSortThreads;
+  constexpr int kCounts = 8;  // in flight
   __shared__ int32_t places[kSortWaves][kDigits];
   __shared__ int32_t sums[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
   bool on[W];
 #pragma unroll
   for (int u = 0; u < W; ++u) {
-    const int32_t i = blockIdx.x * kSortBlock + wave * 64 * W + u * 64 + lane;
+    const int32_t i = blockIdx.x * (kSortThreads * W) + wave * 64 * W + u * 64 + lane;
     on[u] = i < N;
     const int32_t at = on[u] ? i : N - 1;
     row[u] = in.ids != nullptr ? row_of(in.ids[at], V) : in.row[at];
@@ -217,13 +219,23 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
     digit[u] = (row[u] >> shift) & ((1 << bits) - 1);
   }
   // of the thread's digit: tokens of earlier blocks, and of all
-  int32_t earlier = 0, all = 0;
-#pragma unroll 16
-  for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
-    const int32_t n = counts[b * kDigits + tid];
-    all += n;
-    if (b < static_cast<int>(blockIdx.x)) earlier += n;
-  }
+  const auto counted = [&](int b, int end) {
+    int32_t n = 0;
+    for (; b < end; b += kCounts) {
+      int32_t c[kCounts];
+#pragma unroll
+      for (int u = 0; u < kCounts; ++u) c[u] = counts[(b + u < end ? b + u : b) * kDigits + tid];
+      if (b + kCounts <= end) {
+#pragma unroll
+        for (int u = 0; u < kCounts; ++u) n += c[u];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kCounts; ++u) n += b + u < end ? c[u] : 0;
+      }
+    }
+    return n;
+  };
+  const int32_t earlier = counted(0, blockIdx.x), all = earlier + counted(blockIdx.x, gridDim.x);
   const int32_t first = exclusive_sum(all, sums);  // its barrier also follows the zeros above
   rank_digits<W>(digit, on, bits, rank, places[wave]);
   __syncthreads();
@@ -460,6 +472,8 @@ __device__ __forceinline__ bool crosses(const int32_t* sid, int32_t total, int P
   const int64_t end = (q + 1) * P;
   return end < total && sid[end] == id;
 }
+// Lanes before the first that is not set.
+__device__ __forceinline__ int leading_ones(uint64_t m) { return ~m == 0 ? 64 : __builtin_ctzll(~m); }
 // Whether the row of a piece's last position began in an earlier piece.
 __device__ __forceinline__ bool came_in(const int32_t* sid, int P, int64_t q) {
   const int64_t p0 = q * P;
@@ -534,15 +548,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void dlvm_embedding_join_kernel(
   const int back = __builtin_ctzll(~__ballot(in));
   if (back >= kJoinLong) return;  // found by an earlier workgroup
   const int64_t p = q - back;
+  // the first end that the row does not cross, by 64 pieces, then one by one
   int more = 1;
-  for (;;) {
-    const uint64_t stop = ~__ballot(crosses(sid, total, P, p + more + lane, id));
-    if (stop != 0) {
-      more += __builtin_ctzll(stop);
-      break;
-    }
-    more += 64;
-  }
+  for (int far = 64; far == 64; more += 64 * far)
+    far = leading_ones(__ballot(crosses(sid, total, P, p + more + 64 * lane + 63, id)));
+  more += leading_ones(__ballot(crosses(sid, total, P, p + more + lane, id)));
   if (more <= kJoinLong) return;
   const int parts = more + 1, each = (parts + kJoinWaves - 1) / kJoinWaves;
   const int from = wave * each, to = from + each < parts ? from + each : parts;
@@ -569,6 +579,15 @@ int piece_len(int64_t width, int64_t tokens) {
   return waves >= 64 * 2048 ? 64 : waves >= 32 * 2048 ? 32 : 16;
 }
 
+// Tokens of a block to a thread: a block's place in the sort waits for the counts of all
+// blocks, so they grow with the tokens (us to place 20000 tokens with one, two and four: 6.8,
+// 7.4 and 10.4, 65536: 10.3, 9.2 and 10.5, 200001: two 15.6, four 13.9).
+int sort_width(int64_t n) { return n <= (1 << 15) ? 1 : n <= (1 << 17) ? 2 : 4; }
+int sort_blocks(int64_t n) {
+  const int64_t block = int64_t(kSortThreads) * sort_width(n);
+  return static_cast<int>((n + block - 1) / block);
+}
+
 // Workspace of a gradient call: pairs (row, token) before and after a pass, counts, partial sums.
 struct GradWs {
   size_t row[2], tok[2], counts, head, tail, total;
@@ -587,7 +606,7 @@ GradWs grad_ws(int64_t width, int64_t tokens) {
     w.tok[i] = (2 * i + 1) * list;
   }
   w.counts = 4 * list;
-  w.head = w.counts + static_cast<size_t>((w.chunk + kSortBlock - 1) / kSortBlock) * kDigits * 4;
+  w.head = w.counts + static_cast<size_t>(sort_blocks(w.chunk)) * kDigits * 4;
   w.tail = w.head + up(static_cast<size_t>(w.pieces) * width * 4);
   w.total = w.tail + up(static_cast<size_t>(w.pieces) * width * 4);
   return w;
@@ -611,14 +630,18 @@ int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t*
                   digit_bits, share, ids, list(w.row[0]), list(w.tok[0]), dtable);
     return 0;
   }
-  const dim3 blocks(static_cast<uint32_t>((n + kSortBlock - 1) / kSortBlock));
+  const dim3 blocks(static_cast<uint32_t>(sort_blocks(n)));
+  const int width = sort_width(n);
+  const auto count = width == 1   ? dlvm_embedding_count_kernel<1>
+                     : width == 2 ? dlvm_embedding_count_kernel<2> : dlvm_embedding_count_kernel<4>;
+  const auto place = width == 1   ? dlvm_embedding_place_kernel<1>
+                     : width == 2 ? dlvm_embedding_place_kernel<2> : dlvm_embedding_place_kernel<4>;
   int to = 0;
   for (int shift = 0; shift < bits; shift += digit_bits, to ^= 1) {
     const SortIn in = shift == 0 ? SortIn{ids, nullptr, nullptr}
                                  : SortIn{nullptr, list(w.row[to ^ 1]), list(w.tok[to ^ 1])};
-    launch_kernel(dlvm_embedding_count_kernel, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits,
-                  in, list(w.counts));
-    launch_kernel(dlvm_embedding_place_kernel, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits, in,
+    launch_kernel(count, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits, in, list(w.counts));
+    launch_kernel(place, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits, in,
                   static_cast<const int32_t*>(list(w.counts)), list(w.row[to]), list(w.tok[to]));
   }
   return to ^ 1;
