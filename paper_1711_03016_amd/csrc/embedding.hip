@@ -89,7 +89,8 @@ __global__ __launch_bounds__(256) void dlvm_embedding_kernel(uint32_t V, int64_t
 // blocks. Counts are whole numbers, so nothing depends on an order of execution, and a
 // frequent id costs no more than others. Each wave of a block owns consecutive
 // tokens; the lanes of one digit find each other by a ballot to each of its bits. Up to
-// kSmallSort tokens are sorted by one workgroup in LDS. Ids outside the table are taken as
+// kSmallSort tokens are sorted by one workgroup in LDS, beside which others zero the rows
+// without a token (8000 tokens of 32000 x 1024: gradient 39 us, 54 by digits). Ids outside the table are taken as
 // V, one more than the last row: they come last and are left out of the sums. (Choosing a
 // row's tokens from all ids, one workgroup to some rows and without a sort, took 52 us for
 // 200001 tokens of 1021 rows, for the sake of the most frequent row alone.)
@@ -573,7 +574,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void dlvm_embedding_join_kernel(
 }
 
 // Positions of a piece. Long pieces store and read fewer partial sums; short ones keep
-// enough waves in flight when tokens are few.
+// enough waves in flight when tokens are few: 65536 tokens of 1024 columns take a join of 20 us
+// in pieces of 16, 8.6 in pieces of 64; 4099 of 1001 sums of 11.7 us and 24.
 int piece_len(int64_t width, int64_t tokens) {
   const int64_t waves = tokens * ((width + 511) / 512);
   return waves >= 64 * 2048 ? 64 : waves >= 32 * 2048 ? 32 : 16;
@@ -654,7 +656,8 @@ void lookup(int64_t V, int64_t E, int64_t N, const void* table, const int32_t* i
   const int64_t step = (int64_t(1) << 30) / chunks / 4 * 4;  // tokens of one launch (ids stay aligned)
   for (int64_t i0 = 0; i0 < N; i0 += step) {
     const int64_t n = N - i0 < step ? N - i0 : step, total = n * chunks;
-    // every compute unit has eight workgroups before a thread takes a second vector
+    // every compute unit has eight workgroups before a thread takes a second vector; 65536
+    // rows of 1024 bf16 take 51 us with four to a thread, 75 with one
     int64_t blocks = (total + 255) / 256;
     if (blocks > 2048) blocks = (blocks + kLookupUnroll - 1) / kLookupUnroll;
     launch_kernel(dlvm_embedding_kernel<T, VEC>, dim3(static_cast<uint32_t>(blocks)), dim3(256), s,
@@ -685,7 +688,8 @@ void sum_pieces(const Chunk& c, const T* dout, hipStream_t s) {
                 static_cast<int>(sum_blocks), c.n, c.tok, c.row, dout, c.scale, c.add, c.head, c.tail, c.dtable);
 }
 
-// The widest vector that divides the row, and as many to a lane as leave none idle.
+// The widest vector that divides the row, and as many to a lane as leave none idle (160
+// columns: 20.6 us with vectors of two in two slabs, 22.0 with vectors of four on 40 lanes).
 template <typename T> void sum_pieces_any(const Chunk& c, const T* dout, hipStream_t s) {
   const int64_t E = c.E;
   auto f = E % 4 == 0 && E >= 512 ? sum_pieces<T, 4, 2>
