@@ -258,7 +258,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   work_of<MODE>(chain, wave, block, tile);
   if (MODE == CHAINED && block >= chain.blocks) return;
   const Place p = place_of(tile, lane, k);
-  if (MODE == ALONE && !p.on) return;
+  if (MODE == ALONE && __ballot(p.on) == 0) return;  // whole waves: the others compare their lengths
   const int32_t begin = block * (NW * U);
   const int32_t T = static_cast<int32_t>(k.T);
   const int32_t end = MODE != CHAINED || T - begin < NW * U ? T : begin + NW * U;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
   const int block = neighbours(cut.tiles);
   const int s = static_cast<int>(blockIdx.x) / cut.tiles;
   const Place p = place_of(MODE == ALONE ? block * 4 + wave : block, lane, k);
-  if (MODE == ALONE && !p.on) return;
+  if (MODE == ALONE && __ballot(p.on) == 0) return;  // whole waves: the others compare their lengths
   const int64_t N = k.B * k.H;
   const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;

@@ -532,7 +532,9 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_join_kernel(TokenScores
 
 // ---------------------------------------------------------------------------
 // Gradient: with p = exp(y - lse) one pass over the logits, -p (dlogp + dentropy (log p + H))
-// and dlogp more at the token. NT threads take a stretch of a row.
+// and dlogp more at the token. NT threads take a stretch of a row: a wave where the row is
+// short (16384 rows of 100 bf16 10 us, 22 with 256 threads, of 1000 14 and 22), else a
+// workgroup (2048 rows of 50001 float32 133 us, 141 with waves).
 // ---------------------------------------------------------------------------
 struct ScoresGrad {
   int64_t rows, classes;
@@ -651,7 +653,7 @@ constexpr int64_t kFourBytes = 96 << 10;  // if it has up to so many bytes
 constexpr int64_t kCutRow = 32768;      // classes from which a row is cut into parts,
 constexpr int64_t kCutPlain = 98304;    // or these without alternatives,
 constexpr int64_t kCutRows = 128;       // where there are fewer rows
-constexpr int64_t kPartLen = 4096;      // classes of a part at least
+constexpr int64_t kPartLen = 4096;      // classes of a part at least (as fast with 8192)
 constexpr int64_t kBlocks = 512;        // workgroups that fill the GPU
 constexpr int64_t kTurn = 1 << 22;      // workgroups of a launch (its threads are counted in 32 bits)
 
