@@ -112,20 +112,24 @@ __device__ __forceinline__ int bits_below(uint64_t m) {
                                    __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
 }
 
-// Ranks of W vectors of 64 digits of `bits` bits (lanes `on`) among the equal ones of the wave so
-// far, whose counts are kept in `counts`.
+// Ranks of W vectors of 64 digits (lanes `on`) among the equal ones of the wave so far, whose
+// counts are kept in `counts`.
 template <int W>
-__device__ __forceinline__ void rank_digits(const int32_t (&digit)[W], const bool (&on)[W], int bits,
+__device__ __forceinline__ void rank_digits(const int32_t (&digit)[W], const bool (&on)[W],
                                             int32_t (&rank)[W], volatile int32_t* counts) {
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    uint64_t same = __ballot(on[i]);
-    if (same == 0) break;  // the vectors behind the last token
-    for (int b = 0; b < bits; ++b) {
-      const bool bit = (digit[i] >> b) & 1;
-      const uint64_t set = __ballot(bit);
-      same &= bit ? set : ~set;
+    const uint64_t valid = __ballot(on[i]);
+    if (valid == 0) break;  // the vectors behind the last token
+    uint32_t low = static_cast<uint32_t>(valid), high = static_cast<uint32_t>(valid >> 32);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+      const int32_t bit = __builtin_amdgcn_sbfe(digit[i], b, 1);  // 0 or -1
+      const uint64_t set = __ballot(bit < 0);
+      low &= ~(static_cast<uint32_t>(set) ^ bit);
+      high &= ~(static_cast<uint32_t>(set >> 32) ^ bit);
     }
+    const uint64_t same = static_cast<uint64_t>(high) << 32 | low;
     const int before = bits_below(same);
     if (on[i]) {
       const int32_t so_far = counts[digit[i]];
@@ -238,7 +242,7 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
   };
   const int32_t earlier = counted(0, blockIdx.x), all = earlier + counted(blockIdx.x, gridDim.x);
   const int32_t first = exclusive_sum(all, sums);  // its barrier also follows the zeros above
-  rank_digits<W>(digit, on, bits, rank, places[wave]);
+  rank_digits<W>(digit, on, rank, places[wave]);
   __syncthreads();
   int32_t n[kSortWaves];
   take_counts(places, n);
@@ -305,33 +309,32 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < W; ++u) digit[u] = (row[u] >> shift) & ((1 << digit_bits) - 1);
-    rank_digits<W>(digit, on, digit_bits, rank, places[wave]);
+    rank_digits<W>(digit, on, rank, places[wave]);
     __syncthreads();
     int32_t n[kSortWaves];
     const int32_t all = take_counts(places, n);
     place_waves(places, n, exclusive_sum(all, sums));
     __syncthreads();
-    const bool last = shift + digit_bits >= bits;
 #pragma unroll
     for (int u = 0; u < W; ++u)
       if (on[u]) {
         const int32_t at = places[wave][digit[u]] + rank[u];
-        if (last) {
-          row_out[at] = row[u];
-          tok_out[at] = tok[u];
-        } else {
-          rows[at] = row[u];
-          toks[at] = static_cast<uint16_t>(tok[u]);
-        }
+        rows[at] = row[u];
+        toks[at] = static_cast<uint16_t>(tok[u]);
       }
-    if (last) return;
     __syncthreads();
+    if (shift + digit_bits >= bits) break;
 #pragma unroll
     for (int u = 0; u < W; ++u)
       if (on[u]) {
         row[u] = rows[first + u * 64];
         tok[u] = toks[first + u * 64];
       }
+  }
+  // from LDS in order: one compute unit takes a cycle for each line that a wave stores to
+  for (int32_t i = tid; i < N; i += kSortThreads) {
+    row_out[i] = rows[i];
+    tok_out[i] = toks[i];
   }
 }
 
