@@ -148,3 +148,48 @@ def test_gradient_takes_differences():
     want = (d.double() * g.double()).sum().item()
     # linear: the difference is exact but for the roundings of N * E terms of about 3
     assert abs(outs[0] - outs[1] - want) <= N * E * 4 * 4 * U32
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("how", ["zipf", "one", "few"])
+@pytest.mark.parametrize("V,E,N", [(700, 20, 8193), (70001, 6, 32769), (1025, 12, 131073), (3000, 9, 270000)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_each_sort(dtype, how, V, E, N, accumulate):
+    """About the numbers of tokens at which the sort changes, rows of thousands of pieces; sums
+    of small whole numbers, which float32 holds exactly in any order."""
+    import torch
+    r = _rng(5, V, E, N)
+    ids = _ids(r, V, N, how)
+    dout = r.integers(-2, 3, (N, E)).astype(np.float32)
+    base = r.integers(-9, 10, (V, E)).astype(np.float32)
+    ref = np.stack([np.bincount(ids[ids >= 0], weights=dout[ids >= 0, c], minlength=V) for c in range(E)], axis=1)
+    ws = torch.full((dl.embedding_backward_ws_bytes(V, E, N),), 255, dtype=torch.uint8, device=device())
+    d = to_dev(base) if accumulate else torch.full((V, E), float("nan"), device=device())
+    dl.embedding_backward(dtype, V, E, N, _dev_ids(ids), to_dev(dout, dtype), 2.0, accumulate, d, ws)
+    assert (to_np(d) == 2 * ref + (base if accumulate else 0)).all()
+
+
+def test_offsets_beyond_32_bits():
+    """Tables of more than 2^31 elements: rows at their ends looked up, and summed."""
+    import torch
+    V, E = 1_060_000, 2048
+    assert V * E > 1 << 31
+    r = _rng(6)
+    rows = np.array([0, 1, V // 2, 1048576, V - 2, V - 1], np.int32)
+    ids = np.concatenate([rows, rows[::-1], [-1, V]]).astype(np.int32)
+    values = quant(r.standard_normal((len(rows), E)).astype(np.float32), "bf16")
+    table = torch.zeros((V, E), dtype=torch.bfloat16, device=device())
+    table[torch.from_numpy(rows.astype(np.int64)).to(device())] = to_dev(values.astype(np.float32), "bf16")
+    out = torch.empty((len(ids), E), dtype=torch.bfloat16, device=device())
+    dl.embedding_forward("bf16", V, E, len(ids), table, _dev_ids(ids), 2.0, out)
+    got = to_np(out)
+    assert (got[:6] == 2 * values).all() and (got[6:12] == 2 * values[::-1]).all()
+    assert (got[12] == 0).all() and np.isnan(got[13]).all()
+    del table
+    d = torch.full((V, E), float("nan"), device=device())
+    ws = torch.empty(dl.embedding_backward_ws_bytes(V, E, len(ids)), dtype=torch.uint8, device=device())
+    dl.embedding_backward("bf16", V, E, len(ids), _dev_ids(ids), out, 1.0, False, d, ws)
+    at = torch.from_numpy(rows.astype(np.int64)).to(device())
+    assert (to_np(d[at]) == 4 * values).all()
+    d[at] = 0.0
+    assert not d.any()

@@ -287,3 +287,39 @@ def test_gradient_of_padding_is_zero(types, V, entropy):
     sub = lambda v: None if v is None else v[keep]  # noqa: E731
     ref = oracle.token_scores_vjp(q, tokens[keep], 1.0, dlogp[keep], sub(dent))
     _same(got[keep], ref, _grad_tol(q, tokens[keep], 1.0, dlogp[keep], sub(dent), out, ref), "dlogits")
+
+
+@pytest.mark.parametrize("top", [0, 5])
+def test_offsets_beyond_32_bits(top):
+    """More than 2^31 logits: the last rows' scores and gradient as those of a call of them alone."""
+    import torch
+    R, V = 53_000, 41_000
+    assert R * V > 1 << 31
+    g = torch.Generator(device=device()).manual_seed(11)
+    z = torch.zeros((R, V), dtype=torch.bfloat16, device=device())
+    z[-8:] = torch.randn((8, V), generator=g, device=device()).to(torch.bfloat16)
+    tokens = torch.arange(R, dtype=torch.int32, device=device()) % V
+    dlogp = torch.randn(R, generator=g, device=device())
+
+    def scores(z, tokens, dlogp, out):
+        n = z.shape[0]
+        o = [torch.empty(n, device=device()) for _ in range(3)]
+        ids = torch.empty((n, top), dtype=torch.int32, device=device()) if top else None
+        tlp = torch.empty((n, top), device=device()) if top else None
+        dl.token_logprobs("bf16", n, V, z, V, 1.0, tokens, *o, top, ids, tlp)
+        dl.token_logprobs_backward("bf16", "bf16", n, V, z, V, 1.0, tokens, o[1], o[2], dlogp, None, out, V)
+        return o + ([ids, tlp] if top else []) + [out]
+
+    few = z[-8:].clone()
+    want = scores(few, tokens[-8:].clone(), dlogp[-8:].clone(), torch.empty_like(few))
+    got = scores(z, tokens, dlogp, z)                       # in place
+    t = (V / 64 + 64 + 8 * 6) * U32                         # |y| of a normal of these rows below 6
+    for a, b in zip(got[:3], want[:3]):
+        assert (a[-8:] - b).abs().max() <= 4 * t * (1 + np.log(V))
+        assert a.isfinite().all()
+    assert (got[1][:-8] - np.log(V)).abs().max() <= 4 * t
+    if top:
+        assert torch.equal(got[3][-8:], want[3])
+        assert (got[3][0].cpu() == torch.arange(top)).all()
+    d, ref = got[-1][-8:].float(), want[-1].float()
+    assert ((d - ref).abs() <= 2 * (2.0 ** -8 + 8 * t) * ref.abs() + 1e-37).all()
