@@ -89,11 +89,13 @@ __global__ __launch_bounds__(256) void dlvm_embedding_kernel(uint32_t V, int64_t
 // blocks. Counts are whole numbers, so nothing depends on an order of execution, and a
 // frequent id costs no more than others. Each wave of a block owns consecutive
 // tokens; the lanes of one digit find each other by a ballot to each of its bits. Up to
-// kSmallSort tokens are sorted by one workgroup in LDS, beside which others zero the rows
-// without a token (8000 tokens of 32000 x 1024: gradient 39 us, 54 by digits). Ids outside the table are taken as
-// V, one more than the last row: they come last and are left out of the sums. (Choosing a
-// row's tokens from all ids, one workgroup to some rows and without a sort, took 52 us for
-// 200001 tokens of 1021 rows, for the sake of the most frequent row alone.)
+// kSmallSort tokens are placed by one launch that counts those before each, beside which other
+// workgroups zero the rows without a token (8000 tokens of 32000 x 1024: gradient 39 us, 54 by
+// digits; 1000 tokens placed in 5.2 us, 6.8 by one workgroup and digits in LDS, 8000 in 14.8 and
+// 15.8). Ids outside the table are taken as V, one more than the last row: they come last and
+// are left out of the sums. (Choosing a row's tokens from all ids, one workgroup to some rows
+// and without a sort, took 52 us for 200001 tokens of 1021 rows, for the sake of the most
+// frequent row alone.)
 // ---------------------------------------------------------------------------
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
@@ -266,20 +268,22 @@ __device__ __forceinline__ void zero_row(float* __restrict__ row, int64_t E) {
   for (; c < E; ++c) row[c] = 0.0f;
 }
 
-// The first workgroup sorts; each of the others zeroes the absent ones of `share` rows, which it
+// The sort of few tokens: a token's place is the number of tokens that come before it. Each of
+// the first `blocks` workgroups places 64 tokens, one to a lane, whose waves compare them with
+// equal shares of all ids; each of the others zeroes the absent ones of `share` rows, which it
 // finds by reading all ids.
+constexpr int kMarks = 1 << 16;  // rows at most
+
 __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
-    int32_t V, int64_t E, int32_t N, int bits, int digit_bits, int share, const int32_t* __restrict__ ids,
+    int32_t V, int64_t E, int32_t N, int blocks, int share, const int32_t* __restrict__ ids,
     int32_t* __restrict__ row_out, int32_t* __restrict__ tok_out, float* __restrict__ dtable) {
-  constexpr int W = kSmallSort / kSortThreads;
-  __shared__ int32_t places[kSortWaves][kDigits];
-  __shared__ int32_t rows[kSmallSort];
-  __shared__ uint16_t toks[kSmallSort];
-  __shared__ int32_t sums[kSortWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (blockIdx.x > 0) {
-    uint8_t* present = reinterpret_cast<uint8_t*>(places);
-    const int32_t r0 = static_cast<int32_t>(blockIdx.x - 1) * share;
+  __shared__ uint8_t present[kMarks];
+  __shared__ int32_t before[kSortWaves][64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int own = static_cast<int>(blockIdx.x);
+  if (own >= blocks) {
+    const int32_t r0 = (own - blocks) * share;
     const int32_t n = V - r0 < share ? V - r0 : share;
     for (int r = tid; r < n; r += kSortThreads) present[r] = 0;
     __syncthreads();
@@ -292,49 +296,32 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
       if (present[r] == 0) zero_row(dtable + static_cast<int64_t>(r0 + r) * E, E);
     return;
   }
-  const int span = (N + kSortThreads - 1) / kSortThreads * 64;  // tokens of a wave
-  const int first = wave * span + lane;
-  int32_t row[W], tok[W], digit[W], rank[W];
-  bool on[W];
+  const int32_t tok = own * 64 + lane;
+  const int32_t row = row_of(ids[tok < N ? tok : N - 1], V);
+  int32_t n = 0;
+  for (int c = wave; c < blocks; c += kSortWaves) {
+    const int32_t* chunk = ids + c * 64;
+    const int count = N - c * 64 < 64 ? N - c * 64 : 64;
+    if (c == own) {  // of equal ids the earlier lane's comes first
+      for (int j = 0; j < count; ++j) n += __builtin_amdgcn_readlane(row, j) < row + (j < lane ? 1 : 0);
+    } else {
+      const int32_t bound = row + (c < own ? 1 : 0);
+      if (count == 64) {
 #pragma unroll
-  for (int u = 0; u < W; ++u) {
-    const int32_t i = first + u * 64;
-    on[u] = u * 64 < span && i < N;
-    row[u] = row_of(ids[on[u] ? i : N - 1], V);
-    tok[u] = i;
-  }
-  for (int shift = 0;; shift += digit_bits) {
-#pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) places[w][tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < W; ++u) digit[u] = (row[u] >> shift) & ((1 << digit_bits) - 1);
-    rank_digits<W>(digit, on, rank, places[wave]);
-    __syncthreads();
-    int32_t n[kSortWaves];
-    const int32_t all = take_counts(places, n);
-    place_waves(places, n, exclusive_sum(all, sums));
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < W; ++u)
-      if (on[u]) {
-        const int32_t at = places[wave][digit[u]] + rank[u];
-        rows[at] = row[u];
-        toks[at] = static_cast<uint16_t>(tok[u]);
+        for (int j = 0; j < 64; ++j) n += row_of(chunk[j], V) < bound;
+      } else {
+        for (int j = 0; j < count; ++j) n += row_of(chunk[j], V) < bound;
       }
-    __syncthreads();
-    if (shift + digit_bits >= bits) break;
-#pragma unroll
-    for (int u = 0; u < W; ++u)
-      if (on[u]) {
-        row[u] = rows[first + u * 64];
-        tok[u] = toks[first + u * 64];
-      }
+    }
   }
-  // from LDS in order: one compute unit takes a cycle for each line that a wave stores to
-  for (int32_t i = tid; i < N; i += kSortThreads) {
-    row_out[i] = rows[i];
-    tok_out[i] = toks[i];
+  before[wave][lane] = n;
+  __syncthreads();
+  if (wave == 0 && tok < N) {
+    int32_t at = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) at += before[w][lane];
+    row_out[at] = row;
+    tok_out[at] = tok;
   }
 }
 
@@ -617,8 +604,8 @@ GradWs grad_ws(int64_t width, int64_t tokens) {
   return w;
 }
 
-// The call's n tokens sorted by row; returns which of the two lists holds them. A sort by one
-// workgroup leaves the GPU to others that zero the rows without a token (`zero`).
+// The call's n tokens sorted by row; returns which of the two lists holds them. The launch that
+// sorts few leaves room for workgroups that zero the rows without a token (`zero`).
 int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t* ids, char* ws, bool zero,
                 float* dtable, hipStream_t s) {
   const auto list = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
@@ -627,12 +614,12 @@ int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t*
   const int passes = (bits + kDigitBits - 1) / kDigitBits, digit_bits = (bits + passes - 1) / passes;
   if (n <= kSmallSort) {
     // a workgroup to each other compute unit, of 64 rows at least and those it can mark at most
-    constexpr int marks = sizeof(int32_t) * kSortWaves * kDigits;
-    const int even = (V + 254) / 255;
-    const int share = even < 64 ? 64 : even < marks ? even : marks;
+    const int blocks = (n + 63) / 64;
+    const int even = (V + 254 - blocks) / (255 - blocks);
+    const int share = even < 64 ? 64 : even < kMarks ? even : kMarks;
     const uint32_t others = zero ? static_cast<uint32_t>((V + share - 1) / share) : 0;
-    launch_kernel(dlvm_embedding_sort_kernel, dim3(1 + others), dim3(kSortThreads), s, V, E, n, bits,
-                  digit_bits, share, ids, list(w.row[0]), list(w.tok[0]), dtable);
+    launch_kernel(dlvm_embedding_sort_kernel, dim3(blocks + others), dim3(kSortThreads), s, V, E, n, blocks,
+                  share, ids, list(w.row[0]), list(w.tok[0]), dtable);
     return 0;
   }
   const dim3 blocks(static_cast<uint32_t>(sort_blocks(n)));
