@@ -464,7 +464,9 @@ dlvm_status dlvm_sgd(int32_t dtype, int64_t n, void* params, float* master,
  * Sequence operators: token embeddings, the gated linear recurrence and the
  * scoring of tokens, the steps that a recurrent language model needs beside
  * the dense layers. Step-level calls like the ones above. Token ids are int32;
- * -1 stands for "no token" (padding).
+ * -1 stands for "no token" (padding). A workspace serves one call at a time:
+ * calls that may overlap (on other streams, in graphs replayed at once) have
+ * workspaces of their own; it needs no initial contents and keeps none.
  * ------------------------------------------------------------------------- */
 
 /* Rows of a table: out[i, :] = scale * table[ids[i], :] (the dense layer of
@@ -550,7 +552,8 @@ dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps,
  * 0 and no part in the entropy. A row whose y are all below -1e30 is masked
  * everywhere: it has lse = logp = top_logp = -infinity and entropy 0. A row
  * with a NaN or +infinity has NaN for lse, logp, entropy and top_logp; a NaN
- * counts as -infinity in the order of top_ids. `ws` (dlvm_token_logprobs_ws_bytes, or NULL) lets a call of few
+ * counts as -infinity in the order of top_ids. A y whose product overflows
+ * float32 is not what the calls are for. `ws` (dlvm_token_logprobs_ws_bytes, or NULL) lets a call of few
  * rows cut them into parts that run side by side; with NULL no row is cut. */
 enum { DLVM_TOP_MAX = 32 };
 size_t dlvm_token_logprobs_ws_bytes(int64_t rows, int64_t classes, int32_t top);
