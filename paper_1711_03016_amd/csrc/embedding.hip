@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void dlvm_embedding_kernel(uint32_t V, int64_t
 // frequent id costs no more than others. Each wave of a block owns consecutive
 // tokens; the lanes of one digit find each other by a ballot to each of its bits. Up to
 // kSmallSort tokens are placed by one launch that counts those before each, beside which other
-// workgroups zero the rows without a token (8000 tokens of 32000 x 1024: gradient 39 us, 54 by
+// workgroups zero the table (8000 tokens of 32000 x 1024: gradient 39 us, 54 by
 // digits; 1000 tokens placed in 5.2 us, 6.8 by one workgroup and digits in LDS, 8000 in 14.8 and
 // 15.8). Ids outside the table are taken as V, one more than the last row: they come last and
 // are left out of the sums. (Choosing a row's tokens from all ids, one workgroup to some rows
@@ -270,30 +270,29 @@ __device__ __forceinline__ void zero_row(float* __restrict__ row, int64_t E) {
 
 // The sort of few tokens: a token's place is the number of tokens that come before it. Each of
 // the first `blocks` workgroups places 64 tokens, one to a lane, whose waves compare them with
-// equal shares of all ids; each of the others zeroes the absent ones of `share` rows, which it
-// finds by reading all ids.
-constexpr int kMarks = 1 << 16;  // rows at most
+// equal shares of all ids; each of the others zeroes kZeroQuads vectors of the table, of rows
+// with a token too (leaving those out cost more than it saved: 32003 x 1001 float32 in 23.7 us,
+// now 18.8, 6.8 TB/s).
+constexpr int64_t kZeroQuads = 8 * kSortThreads;
 
 __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
-    int32_t V, int64_t E, int32_t N, int blocks, int share, const int32_t* __restrict__ ids,
+    int32_t V, int64_t E, int32_t N, int blocks, const int32_t* __restrict__ ids,
     int32_t* __restrict__ row_out, int32_t* __restrict__ tok_out, float* __restrict__ dtable) {
-  __shared__ uint8_t present[kMarks];
   __shared__ int32_t before[kSortWaves][64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int own = static_cast<int>(blockIdx.x);
   if (own >= blocks) {
-    const int32_t r0 = (own - blocks) * share;
-    const int32_t n = V - r0 < share ? V - r0 : share;
-    for (int r = tid; r < n; r += kSortThreads) present[r] = 0;
-    __syncthreads();
-    for (int32_t i = tid; i < N; i += kSortThreads) {
-      const uint32_t r = static_cast<uint32_t>(ids[i]) - static_cast<uint32_t>(r0);
-      if (r < static_cast<uint32_t>(n)) present[r] = 1;
+    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const int64_t numbers = V * E, q0 = (own - blocks) * kZeroQuads + tid;
+#pragma unroll
+    for (int u = 0; u < kZeroQuads / kSortThreads; ++u) {
+      const int64_t at = 4 * (q0 + u * kSortThreads);
+      if (at + 4 <= numbers)
+        *reinterpret_cast<float4*>(dtable + at) = zero;
+      else
+        for (int64_t i = at; i < numbers; ++i) dtable[i] = 0.0f;
     }
-    __syncthreads();
-    for (int r = wave; r < n; r += kSortWaves)
-      if (present[r] == 0) zero_row(dtable + static_cast<int64_t>(r0 + r) * E, E);
     return;
   }
   const int32_t tok = own * 64 + lane;
@@ -605,7 +604,7 @@ GradWs grad_ws(int64_t width, int64_t tokens) {
 }
 
 // The call's n tokens sorted by row; returns which of the two lists holds them. The launch that
-// sorts few leaves room for workgroups that zero the rows without a token (`zero`).
+// sorts few leaves room for workgroups that zero the table (`zero`).
 int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t* ids, char* ws, bool zero,
                 float* dtable, hipStream_t s) {
   const auto list = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
@@ -613,13 +612,10 @@ int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t*
   while ((V >> bits) != 0) ++bits;
   const int passes = (bits + kDigitBits - 1) / kDigitBits, digit_bits = (bits + passes - 1) / passes;
   if (n <= kSmallSort) {
-    // a workgroup to each other compute unit, of 64 rows at least and those it can mark at most
     const int blocks = (n + 63) / 64;
-    const int even = (V + 254 - blocks) / (255 - blocks);
-    const int share = even < 64 ? 64 : even < kMarks ? even : kMarks;
-    const uint32_t others = zero ? static_cast<uint32_t>((V + share - 1) / share) : 0;
-    launch_kernel(dlvm_embedding_sort_kernel, dim3(blocks + others), dim3(kSortThreads), s, V, E, n, blocks,
-                  share, ids, list(w.row[0]), list(w.tok[0]), dtable);
+    const int64_t others = zero ? (V * E + 4 * kZeroQuads - 1) / (4 * kZeroQuads) : 0;
+    launch_kernel(dlvm_embedding_sort_kernel, dim3(static_cast<uint32_t>(blocks + others)), dim3(kSortThreads),
+                  s, V, E, n, blocks, ids, list(w.row[0]), list(w.tok[0]), dtable);
     return 0;
   }
   const dim3 blocks(static_cast<uint32_t>(sort_blocks(n)));
