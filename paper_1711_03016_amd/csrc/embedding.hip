@@ -3,10 +3,13 @@
 //
 // The gradient, dtable[v] = scale * sum of dout[i] over the tokens i with id v, uses no
 // floating-point atomics: the tokens are sorted by id, equal pieces of the sorted list are
-// summed (by the launch that zeroes the rows without a token, most of the bytes of a large
-// table), and the sums of rows that run over a piece's end are joined in the order of the
-// pieces.
+// summed, and the sums of rows that run over a piece's end are joined in the order of the
+// pieces. The sort leaves most of the GPU idle, so its launches fill the table with zeros; of a
+// large one, the launch that sums the pieces zeroes the rows without a token instead, most of
+// its bytes.
 #include <math.h>
+
+#include <algorithm>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -103,6 +106,10 @@ constexpr int kSortThreads = kDigits;                // one thread to a digit
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSmallSort = 8 * kSortThreads;
 constexpr int64_t kSortTokens = int64_t(1) << 18;    // tokens of one sort
+// Numbers of a table that is filled beside a sort by digits: 9000 tokens of 131072 x 512
+// float32 take 77 us (lookup too), 88 with the rows without a token zeroed beside the sums,
+// 40000 of 100000 x 301 84 and 90; 65536 of 131072 x 1024 215 and 214.
+constexpr int64_t kFillBeside = int64_t(1) << 26;
 
 __device__ __forceinline__ int32_t row_of(int32_t id, int32_t V) {
   return static_cast<uint32_t>(id) < static_cast<uint32_t>(V) ? id : V;
@@ -177,11 +184,30 @@ __device__ __forceinline__ void place_waves(int32_t (*counts)[kDigits], const in
   }
 }
 
-// Where the tokens of a pass come from: ids (first pass) or pairs sorted by lower digits.
+// kZeroQuads vectors of `numbers` zeros by a workgroup, the b-th.
+constexpr int64_t kZeroQuads = 8 * kSortThreads;
+__device__ __forceinline__ void zero_part(float* __restrict__ to, int64_t numbers, int b) {
+  const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const int64_t q0 = b * kZeroQuads + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < kZeroQuads / kSortThreads; ++u) {
+    const int64_t at = 4 * (q0 + u * kSortThreads);
+    if (at + 4 <= numbers)
+      *reinterpret_cast<float4*>(to + at) = zero;
+    else
+      for (int64_t i = at; i < numbers; ++i) to[i] = 0.0f;
+  }
+}
+
+// Where the tokens of a pass come from: ids (first pass) or pairs sorted by lower digits; the
+// workgroups that sort, and what those behind them zero.
 struct SortIn {
   const int32_t* ids;
   const int32_t* row;
   const int32_t* tok;
+  int blocks;
+  float* zero;
+  int64_t zeros;
 };
 
 // W tokens of a block to each thread.
@@ -190,6 +216,8 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_count_kernel(int3
                                                                             int bits, SortIn in,
                                                                             int32_t* __restrict__ counts) {
   __shared__ int32_t hist[kDigits];
+  if (static_cast<int>(blockIdx.x) >= in.blocks)
+    return zero_part(in.zero, in.zeros, static_cast<int>(blockIdx.x) - in.blocks);
   hist[threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
@@ -212,6 +240,8 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
   __shared__ int32_t places[kSortWaves][kDigits];
   __shared__ int32_t sums[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (static_cast<int>(blockIdx.x) >= in.blocks)
+    return zero_part(in.zero, in.zeros, static_cast<int>(blockIdx.x) - in.blocks);
 #pragma unroll
   for (int w = 0; w < kSortWaves; ++w) places[w][tid] = 0;
   int32_t row[W], tok[W], digit[W], rank[W];
@@ -242,7 +272,7 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_place_kernel(
     }
     return n;
   };
-  const int32_t earlier = counted(0, blockIdx.x), all = earlier + counted(blockIdx.x, gridDim.x);
+  const int32_t earlier = counted(0, blockIdx.x), all = earlier + counted(blockIdx.x, in.blocks);
   const int32_t first = exclusive_sum(all, sums);  // its barrier also follows the zeros above
   rank_digits<W>(digit, on, rank, places[wave]);
   __syncthreads();
@@ -273,8 +303,6 @@ __device__ __forceinline__ void zero_row(float* __restrict__ row, int64_t E) {
 // equal shares of all ids; each of the others zeroes kZeroQuads vectors of the table, of rows
 // with a token too (leaving those out cost more than it saved: 32003 x 1001 float32 in 23.7 us,
 // now 18.8, 6.8 TB/s).
-constexpr int64_t kZeroQuads = 8 * kSortThreads;
-
 __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
     int32_t V, int64_t E, int32_t N, int blocks, const int32_t* __restrict__ ids,
     int32_t* __restrict__ row_out, int32_t* __restrict__ tok_out, float* __restrict__ dtable) {
@@ -282,19 +310,7 @@ __global__ __launch_bounds__(kSortThreads) void dlvm_embedding_sort_kernel(
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int own = static_cast<int>(blockIdx.x);
-  if (own >= blocks) {
-    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const int64_t numbers = V * E, q0 = (own - blocks) * kZeroQuads + tid;
-#pragma unroll
-    for (int u = 0; u < kZeroQuads / kSortThreads; ++u) {
-      const int64_t at = 4 * (q0 + u * kSortThreads);
-      if (at + 4 <= numbers)
-        *reinterpret_cast<float4*>(dtable + at) = zero;
-      else
-        for (int64_t i = at; i < numbers; ++i) dtable[i] = 0.0f;
-    }
-    return;
-  }
+  if (own >= blocks) return zero_part(dtable, V * E, own - blocks);
   const int32_t tok = own * 64 + lane;
   const int32_t row = row_of(ids[tok < N ? tok : N - 1], V);
   int32_t n = 0;
@@ -603,9 +619,9 @@ GradWs grad_ws(int64_t width, int64_t tokens) {
   return w;
 }
 
-// The call's n tokens sorted by row; returns which of the two lists holds them. The launch that
-// sorts few leaves room for workgroups that zero the table (`zero`).
-int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t* ids, char* ws, bool zero,
+// The call's n tokens sorted by row; returns which of the two lists holds them. If the table is
+// to be zeroed (`zero`), its launches may do that, and then say so.
+int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t* ids, char* ws, bool& zero,
                 float* dtable, hipStream_t s) {
   const auto list = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
   int bits = 1;  // of the largest key, V
@@ -616,9 +632,23 @@ int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t*
     const int64_t others = zero ? (V * E + 4 * kZeroQuads - 1) / (4 * kZeroQuads) : 0;
     launch_kernel(dlvm_embedding_sort_kernel, dim3(static_cast<uint32_t>(blocks + others)), dim3(kSortThreads),
                   s, V, E, n, blocks, ids, list(w.row[0]), list(w.tok[0]), dtable);
+    zero = false;
     return 0;
   }
-  const dim3 blocks(static_cast<uint32_t>(sort_blocks(n)));
+  // a table that is not too large is filled beside the sort, an equal part by each launch
+  const int blocks = sort_blocks(n);
+  const int64_t all = zero && V * E <= kFillBeside ? V * E : 0;
+  const int64_t each = ((all + 2 * passes - 1) / (2 * passes) + 3) / 4 * 4;
+  const dim3 grid(static_cast<uint32_t>(blocks + (each + 4 * kZeroQuads - 1) / (4 * kZeroQuads)));
+  if (all > 0) zero = false;
+  int64_t done = 0;
+  const auto with_zeros = [&](SortIn in) {
+    in.blocks = blocks;
+    in.zero = dtable + done;
+    in.zeros = std::min(all - done, each);
+    done += in.zeros;
+    return in;
+  };
   const int width = sort_width(n);
   const auto count = width == 1   ? dlvm_embedding_count_kernel<1>
                      : width == 2 ? dlvm_embedding_count_kernel<2> : dlvm_embedding_count_kernel<4>;
@@ -628,8 +658,8 @@ int sort_tokens(const GradWs& w, int32_t V, int64_t E, int32_t n, const int32_t*
   for (int shift = 0; shift < bits; shift += digit_bits, to ^= 1) {
     const SortIn in = shift == 0 ? SortIn{ids, nullptr, nullptr}
                                  : SortIn{nullptr, list(w.row[to ^ 1]), list(w.tok[to ^ 1])};
-    launch_kernel(count, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits, in, list(w.counts));
-    launch_kernel(place, blocks, dim3(kSortThreads), s, V, n, shift, digit_bits, in,
+    launch_kernel(count, grid, dim3(kSortThreads), s, V, n, shift, digit_bits, with_zeros(in), list(w.counts));
+    launch_kernel(place, grid, dim3(kSortThreads), s, V, n, shift, digit_bits, with_zeros(in),
                   static_cast<const int32_t*>(list(w.counts)), list(w.row[to]), list(w.tok[to]));
   }
   return to ^ 1;
@@ -713,8 +743,9 @@ hipError_t launch_embedding_backward(int dtype, int64_t vocab, int64_t width, in
   for (int64_t t0 = 0; t0 < tokens; t0 += w.chunk) {
     const int32_t n = static_cast<int32_t>(tokens - t0 < w.chunk ? tokens - t0 : w.chunk);
     const bool add = accumulate || t0 > 0;
-    const int at = sort_tokens(w, V, width, n, ids + t0, base, !add, dtable, s);
-    const Chunk c{V, width, n, list(w.row[at]), list(w.tok[at]), scale, add, !add && n > kSmallSort,
+    bool zero = !add;
+    const int at = sort_tokens(w, V, width, n, ids + t0, base, zero, dtable, s);
+    const Chunk c{V, width, n, list(w.row[at]), list(w.tok[at]), scale, add, zero,
                   reinterpret_cast<float*>(base + w.head), reinterpret_cast<float*>(base + w.tail), dtable, w.P};
     if (dtype == F32)
       sum_pieces_any<float>(c, static_cast<const float*>(dout) + t0 * width, s);
