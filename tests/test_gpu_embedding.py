@@ -193,3 +193,22 @@ def test_offsets_beyond_32_bits():
     assert (to_np(d[at]) == 4 * values).all()
     d[at] = 0.0
     assert not d.any()
+
+
+@pytest.mark.parametrize("V,E,N", [(70001, 1000, 9001), (131072, 513, 20000), (40000, 333, 8193), (131071, 513, 77)])
+def test_gradient_of_large_tables(V, E, N):
+    """Tables zeroed beside the sort and beside the sums; sums of whole numbers, exact in any order."""
+    import torch
+    r = _rng(8, V, E, N)
+    ids = _ids(r, V, N, "zipf")
+    ids[::50] = -1
+    ids[-1] = V - 1
+    dout = torch.from_numpy(r.integers(-2, 3, (N, E)).astype(np.float32)).to(device())
+    have = torch.from_numpy((ids >= 0).astype(np.int64).nonzero()[0]).to(device())
+    ref = torch.zeros((V, E), device=device())
+    ref.index_add_(0, torch.from_numpy(ids[ids >= 0].astype(np.int64)).to(device()), dout[have])
+    ws = torch.full((dl.embedding_backward_ws_bytes(V, E, N),), 255, dtype=torch.uint8, device=device())
+    d = torch.full((V * E + GUARD,), 7.0, device=device())
+    dl.embedding_backward("f32", V, E, N, _dev_ids(ids), dout, 1.0, False, d, ws)
+    assert torch.equal(d[:V * E].view(V, E), ref)
+    assert (d[V * E:] == 7.0).all()
