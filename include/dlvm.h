@@ -524,11 +524,13 @@ dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, 
 /* Gradient of the recurrence: dhs (row stride lddh, `dtype`; NULL: zeros) holds
  * the adjoints of hs and dhT (float32; NULL: zeros) that of the last state; one
  * of them is given. z, x, h0, lens as in the forward call and hs as it wrote
- * it (the states between are recomputed from a few of its rows). Writes dz and
- * dx (strides lddz, lddx, `dtype`; they may be the two halves of one buffer)
- * and, unless NULL, dh0 (float32 [batch, width]; it may be dhT). Rows t >=
- * lens[b] of dz and dx are zero; those of dhs are not used. Outputs must not
- * overlap inputs otherwise. */
+ * it. The states are float32 here too: those between are recomputed from a few
+ * rows of a float32 hs, and all of them from z, x and h0 where hs is bf16 (its
+ * rows are rounded, and h - x may be smaller than that). Writes dz and dx
+ * (strides lddz, lddx, `dtype`; they may be the two halves of one buffer, and
+ * hold other values while the call runs) and, unless NULL, dh0 (float32 [batch,
+ * width]; it may be dhT). Rows t >= lens[b] of dz and dx are zero; those of dhs
+ * are not used. Outputs must not overlap inputs otherwise. */
 dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps, int64_t batch,
                                      int64_t width, const void* z, int64_t ldz, const void* x,
                                      int64_t ldx, const float* h0, const int32_t* lens,

@@ -15,12 +15,11 @@
 //    from what the workgroups of earlier blocks have published, and publishes the state
 //    after it. Every tensor is read once.
 //  - SHARED in segments of time, the gradient of few states and many steps: a first launch
-//    sums every segment up, and the second starts each from the sums after it. That reads
-//    two of five tensors a second time, from the Infinity Cache as far as they fit: the
-//    second launch begins with the segments that the first read last. (Chained, the gradient's
-//    blocks are too short for the waiting: its registers hold twelve steps of a wave, 110
-//    against 101 us for T = 4096, 8192 states of bf16, where the forward call's 32 steps take
-//    56 us chained and 74 in segments.)
+//    sums every segment up, and the second starts each from the sums after it (and before it,
+//    where it recomputes the states). That reads z, dhs and, for the states, x again, from the
+//    Infinity Cache as far as they fit. (Chained, the gradient's blocks are too short for the
+//    waiting: its registers hold twelve steps of a wave, where the forward call's 32 steps
+//    take 56 us chained and 74 in segments, T = 4096, 8192 states of bf16.)
 // What bounds them is memory; the arithmetic (two transcendental functions to an element)
 // takes about half of what the vector units could do in that time.
 #include <math.h>
@@ -52,13 +51,15 @@ __device__ __forceinline__ int32_t length_of(const int32_t* lens, int32_t b, int
   return n < 0 ? 0 : n > T ? static_cast<int32_t>(T) : n;
 }
 
-// Segments of time of one call. sums[s * N + j] is the map of segment s for state j.
+// Segments of time of a gradient call. sums[s * N + j] is the map (A, M) of segment s for the
+// adjoint of state j, and A with states[s * N + j] that for the state.
 struct Cut {
   int S;               // segments (1: none)
   int32_t len;         // steps of one
   int tiles;           // workgroups of a segment
-  float* init;         // [N] copy of the first state (the caller's may be overwritten in place)
+  float* init;         // [N] copy of the last adjoint (the caller's may be overwritten in place)
   float2* sums;
+  float* states;       // where the states are recomputed
 };
 
 // ---------------------------------------------------------------------------
@@ -368,8 +369,15 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
 
 // ---------------------------------------------------------------------------
 // Gradient, from the last step backwards. The states before a thread's eight steps are
-// recomputed from the one before the first of them, the only row of hs that it reads.
+// recomputed from the one before the first of them. In float32 that is a row of hs. The rows of
+// bf16 are rounded, and where the state follows the input, h - x is smaller than what they are
+// off by: there a pass forwards through z and x finds those states in float32 first, and keeps
+// each in the two bf16 of dz and dx at its first step until the same thread comes back to it
+// and writes the gradients. (The gradient of 32 steps of 2^20 states takes 84 us with that pass
+// and 70 with the rows of hs, 4096 steps of 8192 states 144 and 102.)
 // ---------------------------------------------------------------------------
+template <typename E> constexpr bool kRecompute = sizeof(E) == 2;
+
 template <typename E, bool COUPLED, int MODE>
 __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_scan_grad_kernel(GatedScan k, Cut cut) {
   constexpr int U = kUnroll, NW = MODE == ALONE ? 1 : kWaves;
@@ -394,18 +402,91 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
 
   const float* first = cut.S > 1 ? cut.init : k.dhT;
   float mu = first != nullptr ? first[p.j] : 0.0f;
-  E z[U] = {}, x[U] = {}, d[U] = {}, before = {};
+  E z[U] = {}, x[U] = {}, d[U] = {};
+  float before = 0.0f;
   // as in the forward call
   const int32_t sure = k.lens == nullptr ? end : wave_min(p.on ? live : end);
   const int32_t over = k.lens == nullptr ? end : wave_max(live);
   const int32_t rounds = over > begin ? (over - begin + NW * U - 1) / (NW * U) : 0;
   const int32_t last = begin + (rounds - 1) * (NW * U);  // first step of the last round
   const int32_t stop = (k.lens == nullptr ? end : wave_max(live > begin ? live : begin + 1)) - 1;
+  int phase = 0;
+  float start = k.h0 != nullptr ? k.h0[p.j] : 0.0f;  // the first state; recomputed, the segment's
+  if constexpr (kRecompute<E>) {
+    for (int q = 0; q < s; ++q) start = fmaf(cut.sums[q * N + p.j].x, start, cut.states[q * N + p.j]);
+    const auto forwards = [&](int32_t t0) {
+      const int32_t from = t0 < stop ? t0 : stop;
+      auto rz = pz.row(from), rx = px.row(from);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        z[u] = pz.in(rz);
+        x[u] = px.in(rx);
+        const bool more = t0 + u < stop;
+        rz += more ? pz.step : 0;
+        rx += more ? px.step : 0;
+      }
+    };
+    const auto park = [&](int32_t t, float h) {
+      const uint32_t bits = __float_as_uint(h);
+      gz.in(gz.row(t)) = static_cast<E>(bits >> 16);
+      gx.in(gx.row(t)) = static_cast<E>(bits);
+    };
+    // a thread that goes through all steps has no need of the last of its rounds
+    const int32_t finish = MODE == ALONE ? last : last + NW * U;
+    float h = start;
+    if (finish > begin) forwards(begin + w * U);
+    for (int32_t t0 = begin; t0 < finish; t0 += NW * U) {
+      const int32_t t = t0 + w * U;
+      float a[U], q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float c;
+        gate(load_as_f32(&z[u]), a[u], c);
+        const float xv = load_as_f32(&x[u]);
+        q[u] = COUPLED ? c * xv : xv;
+      }
+      if (t + U > sure)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (t + u >= live) {
+            a[u] = 1.0f;
+            q[u] = 0.0f;
+          }
+      if (t0 + NW * U < finish) forwards(t + NW * U);
+      if (MODE == ALONE) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) h = a[u] * h + q[u];
+        if (p.on) park(t + U, h);
+      } else {
+        float A = a[0], Q = q[0];
+#pragma unroll
+        for (int u = 1; u < U; ++u) {
+          Q = a[u] * Q + q[u];
+          A *= a[u];
+        }
+        sums[phase][w][lane] = make_float2(A, Q);
+        __syncthreads();
+        float now = h;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+          if (i == w) now = h;
+          const float2 m = sums[phase][i][lane];
+          h = fmaf(m.x, h, m.y);
+        }
+        phase ^= 1;
+        if (p.on && t < end) park(t, now);
+      }
+    }
+  }
   const auto fetch = [&](int32_t t0) {
     if (t0 < begin) return;
     const int32_t from = t0 < stop ? t0 : stop;
     auto rz = pz.row(from), rx = px.row(from), rd = pd.row(from);
-    before = ph.in(ph.row(from > 0 ? from - 1 : 0));
+    if constexpr (kRecompute<E>)
+      before = __uint_as_float(static_cast<uint32_t>(gz.in(gz.row(from))) << 16 |
+                               static_cast<uint32_t>(gx.in(gx.row(from))));
+    else
+      before = ph.in(ph.row(from > 0 ? from - 1 : 0));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       z[u] = pz.in(rz);
@@ -429,11 +510,10 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
       gz.in(gz.row(t)) = store_cast<E>(0.0f);
       gx.in(gx.row(t)) = store_cast<E>(0.0f);
     }
-  int phase = 0;
   for (int32_t t0 = last; t0 >= begin; t0 -= NW * U) {
     const int32_t t = t0 + w * U;
     float a[U], c[U], f[U], dh[U];  // f: dz over the adjoint that passes the gate
-    float prev = t > 0 ? load_as_f32(&before) : k.h0 != nullptr ? k.h0[p.j] : 0.0f;
+    float prev = t > 0 ? before : start;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       gate(load_as_f32(&z[u]), a[u], c[u]);
@@ -504,24 +584,27 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
 }
 
 // ---------------------------------------------------------------------------
-// The map of each segment of the gradient but the first, of the adjoint after it to that
-// before it: the waves take equal stretches of it (read forwards), whose maps are composed
-// from the last.
+// The maps of each segment of the gradient: of the adjoint after it to that before it (but the
+// first) and, where the states are recomputed, of the state before it to that after it (but the
+// last). The waves take equal stretches, read forwards, whose maps are composed.
 // ---------------------------------------------------------------------------
-template <typename E>
+template <typename E, bool COUPLED>
 __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(GatedScan k, Cut cut) {
   constexpr int U = 2 * kUnroll;
+  constexpr bool kStates = kRecompute<E>;
   __shared__ float2 sums[kWaves][64];
+  __shared__ float states[kStates ? kWaves : 1][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  const int s = static_cast<int>(blockIdx.x) / cut.tiles + 1;
+  const int s = static_cast<int>(blockIdx.x) / cut.tiles + (kStates ? 0 : 1);
   const Place p = place_of(static_cast<int>(blockIdx.x) % cut.tiles, lane, k);
   const int32_t T = static_cast<int32_t>(k.T);
   const int32_t begin = s * cut.len;
   const int32_t end = T - begin < cut.len ? T : begin + cut.len;
   const int32_t n = length_of(k.lens, p.b, k.T);
-  const bool has_d = k.dhs != nullptr;
-  const Rows<E> pz(k.z, k.ldz, k.B, p);
+  // what a segment has no need of is read from z, whose rows are read anyway
+  const bool has_d = k.dhs != nullptr && s > 0, has_x = kStates && s < cut.S - 1;
+  const Rows<E> pz(k.z, k.ldz, k.B, p), px(has_x ? k.x : k.z, has_x ? k.ldx : k.ldz, k.B, p);
   const Rows<E> pd(has_d ? k.dhs : k.z, has_d ? k.lddh : k.ldz, k.B, p);
   if (p.on && wave == 0 && s == cut.S - 1) cut.init[p.j] = k.dhT != nullptr ? k.dhT[p.j] : 0.0f;
 
@@ -530,16 +613,18 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
   const int32_t t_end = t_begin + stretch < end ? t_begin + stretch : end;
   const int32_t live = !p.on ? 0 : n < t_end ? n : t_end;
   const int32_t t_live = k.lens == nullptr ? t_end : wave_max(live);  // no step is live in any lane beyond
-  float A = 1.0f, M = 0.0f;
+  float A = 1.0f, M = 0.0f, Q = 0.0f;
   for (int32_t t0 = t_begin; t0 < t_live; t0 += U) {
-    E z[U], d[U];
-    auto rz = pz.row(t0), rd = pd.row(t0);
+    E z[U], x[U], d[U];
+    auto rz = pz.row(t0), rx = px.row(t0), rd = pd.row(t0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       z[u] = pz.in(rz);
+      if (kStates) x[u] = px.in(rx);
       d[u] = pd.in(rd);
       const bool more = t0 + u + 1 < t_live;
       rz += more ? pz.step : 0;
+      rx += more ? px.step : 0;
       rd += more ? pd.step : 0;
     }
 #pragma unroll
@@ -551,18 +636,30 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
       // the adjoint of a step reaches the state before the stretch through the gates up to its own
       A = in ? A * a : A;
       M = in ? fmaf(A, dh, M) : M;
+      if (kStates) {
+        const float xv = load_as_f32(&x[u]);
+        Q = in ? a * Q + (COUPLED ? c * xv : xv) : Q;
+      }
     }
   }
   sums[wave][lane] = make_float2(A, M);
+  if (kStates) states[wave][lane] = Q;
   __syncthreads();
   if (wave == 0 && p.on) {
     float2 m = make_float2(1.0f, 0.0f);
+    const int64_t at = s * (k.B * k.H) + p.j;
 #pragma unroll
     for (int i = kWaves - 1; i >= 0; --i) {
       const float2 o = sums[i][lane];
       m = make_float2(o.x * m.x, fmaf(o.x, m.y, o.y));
     }
-    cut.sums[s * (k.B * k.H) + p.j] = m;
+    cut.sums[at] = m;
+    if (kStates) {
+      float q = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) q = fmaf(sums[i][lane].x, q, states[i][lane]);
+      cut.states[at] = q;
+    }
   }
 }
 
@@ -639,7 +736,7 @@ template <typename E, bool COUPLED> hipError_t forward(const GatedScan& c, void*
 
 template <typename E, bool COUPLED> hipError_t backward(const GatedScan& c, void* ws, hipStream_t s) {
   const int64_t N = c.B * c.H;
-  Cut cut{1, static_cast<int32_t>(c.T), static_cast<int>((N + 63) / 64), nullptr, nullptr};
+  Cut cut{1, static_cast<int32_t>(c.T), static_cast<int>((N + 63) / 64), nullptr, nullptr, nullptr};
   if (alone(c.T, N)) {
     cut.tiles = (cut.tiles + 3) / 4;
     launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, ALONE>, dim3(cut.tiles), dim3(256), s, c, cut);
@@ -650,7 +747,9 @@ template <typename E, bool COUPLED> hipError_t backward(const GatedScan& c, void
   if (cut.S > 1) {
     cut.init = static_cast<float*>(ws);
     cut.sums = reinterpret_cast<float2*>(cut.init + (N + 63) / 64 * 64);
-    launch_kernel(dlvm_gated_scan_sums_kernel<E>, dim3(cut.tiles * (cut.S - 1)), block, s, c, cut);
+    cut.states = reinterpret_cast<float*>(cut.sums + cut.S * N);
+    launch_kernel(dlvm_gated_scan_sums_kernel<E, COUPLED && kRecompute<E>>,
+                  dim3(cut.tiles * (cut.S - (kRecompute<E> ? 0 : 1))), block, s, c, cut);
   }
   launch_kernel(dlvm_gated_scan_grad_kernel<E, COUPLED, SHARED>, dim3(cut.tiles * cut.S), block, s, c, cut);
   return hipGetLastError();
@@ -658,11 +757,12 @@ template <typename E, bool COUPLED> hipError_t backward(const GatedScan& c, void
 
 }  // namespace
 
-size_t gated_scan_ws(int, int64_t T, int64_t B, int64_t H) {
+size_t gated_scan_ws(int dtype, int64_t T, int64_t B, int64_t H) {
   int32_t len = 0;
   const int64_t N = B * H, S = segments(T, N, true, &len);  // as many as without lengths, or more
   const size_t tiles = static_cast<size_t>((N + 63) / 64);
-  size_t bytes = S == 1 ? 256 : tiles * 64 * 4 + static_cast<size_t>(S) * N * 8;
+  const size_t maps = dtype == BF16 ? 12 : 8;  // bytes of a segment's
+  size_t bytes = S == 1 ? 256 : tiles * 64 * 4 + static_cast<size_t>(S) * N * maps;
   if (chained(T, N)) {
     const size_t chain = tiles * (kTicketStride * 4 + static_cast<size_t>(blocks_of(T)) * 64 * 8);
     bytes = chain > bytes ? chain : bytes;
