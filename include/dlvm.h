@@ -554,8 +554,9 @@ dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps,
  * 0 and no part in the entropy. A row whose y are all below -1e30 is masked
  * everywhere: it has lse = logp = top_logp = -infinity and entropy 0. A row
  * with a NaN or +infinity has NaN for lse, logp, entropy and top_logp; a NaN
- * counts as -infinity in the order of top_ids. A y that overflows float32 is
- * not what the calls are for. `ws` (dlvm_token_logprobs_ws_bytes, or NULL)
+ * counts as -infinity in the order of top_ids. A y below the range of float32
+ * (a mask times the scale) counts as -infinity; one above it is not what the
+ * calls are for. `ws` (dlvm_token_logprobs_ws_bytes, or NULL)
  * lets a call of few rows cut them into parts that run side by side; with NULL
  * no row is cut. */
 enum { DLVM_TOP_MAX = 32 };

@@ -86,10 +86,12 @@ __device__ __forceinline__ bool masked_everywhere(const Part& p, float scale) {
 }
 
 // p moved to the maximum m >= p.m, d = (p.m - m) scale log2(e) - r. (Nothing to move where
-// the set is empty, whose d may be infinite.)
+// the set is empty, whose d may be infinite. One of masked classes alone may have a d of the
+// size of the type's lowest value: e is 0 there, and long before d reaches -1e4, so that it is
+// multiplied with a finite number. NaN and +infinity come through in s.)
 __device__ __forceinline__ void move_to(Part& p, float m, float d) {
   const float e = exp2_(d);
-  p.w = p.s == 0.0f ? 0.0f : (p.w + p.s * d) * e;
+  p.w = p.s == 0.0f ? 0.0f : (p.w + p.s * fmaxf(d, -1e4f)) * e;
   p.s = p.s == 0.0f ? 0.0f : p.s * e;
   p.m = m;
 }
