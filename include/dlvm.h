@@ -467,6 +467,9 @@ dlvm_status dlvm_sgd(int32_t dtype, int64_t n, void* params, float* master,
  * -1 stands for "no token" (padding). A workspace serves one call at a time:
  * calls that may overlap (on other streams, in graphs replayed at once) have
  * workspaces of their own; it needs no initial contents and keeps none.
+ * Outputs and the workspace must not overlap inputs or each other, but where a
+ * call says so (DLVM_ERR_INVALID_ARG; rows of one stride may lie between each
+ * other's; of rows of two strides only the first bytes are compared).
  * ------------------------------------------------------------------------- */
 
 /* Rows of a table: out[i, :] = scale * table[ids[i], :] (the dense layer of
@@ -474,7 +477,7 @@ dlvm_status dlvm_sgd(int32_t dtype, int64_t n, void* params, float* master,
  * width] are `dtype`; the product with `scale` is float32, rounded once. A row
  * whose id is -1 is zero; one whose id is any other value outside [0, vocab)
  * is NaN. vocab at most 2^24, width at most 2^20, tokens at most 2^30, scale
- * finite; out must not overlap the table. */
+ * finite. */
 dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens,
                                    const void* table, const int32_t* ids, float scale, void* out,
                                    void* stream);
@@ -503,8 +506,7 @@ dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width,
  * and x may be the two halves of one dense product. z, x, hs are `dtype`;
  * the state is float32 throughout: h0 [batch, width] (NULL: zeros), hT [batch,
  * width] (may be NULL) receives the state after the last step. hT may be h0,
- * updated in place: a call with steps = 1 is one decoding step. Other outputs
- * must not overlap inputs.
+ * updated in place: a call with steps = 1 is one decoding step.
  * lens (NULL: every sequence has `steps` steps) holds `batch` int32 lengths of
  * a padded batch, taken as clamped to [0, steps]: steps t >= lens[b] leave the
  * state as it is, their z and x are not used (whatever they hold) and their hs
@@ -530,7 +532,7 @@ dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, 
  * (strides lddz, lddx, `dtype`; they may be the two halves of one buffer, and
  * hold other values while the call runs) and, unless NULL, dh0 (float32 [batch,
  * width]; it may be dhT). Rows t >= lens[b] of dz and dx are zero; those of dhs
- * are not used. Outputs must not overlap inputs otherwise. */
+ * are not used. */
 dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps, int64_t batch,
                                      int64_t width, const void* z, int64_t ldz, const void* x,
                                      int64_t ldx, const float* h0, const int32_t* lens,

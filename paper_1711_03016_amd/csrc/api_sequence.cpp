@@ -4,6 +4,7 @@
 
 #include <climits>
 #include <cmath>
+#include <initializer_list>
 
 #include "dlvm.h"
 #include "api_common.hpp"
@@ -63,8 +64,58 @@ dlvm_status score_sizes(int32_t dtype, int64_t rows, int64_t classes, int64_t ld
 
 template <typename... P> bool all_aligned16(const P*... p) { return (aligned16(p) && ...); }
 
-// Whether `out` starts where one of the inputs does.
-template <typename... P> bool is_one_of(const void* out, const P*... in) { return ((out == in) || ...); }
+// Where a tensor lies: rows of `row` bytes, `pitch` bytes from one to the next.
+struct Span {
+  const void* at;
+  __int128 rows, row, pitch;
+};
+Span piece(const void* at, int64_t count, size_t size) {
+  const __int128 bytes = static_cast<__int128>(count) * static_cast<int64_t>(size);
+  return Span{at, 1, bytes, bytes};
+}
+Span strided(const void* at, int dtype, int64_t rows, int64_t width, int64_t ld) {
+  const int64_t e = static_cast<int64_t>(elem_size(dtype));
+  if (ld == width) return piece(at, rows * width, elem_size(dtype));
+  return Span{at, rows, static_cast<__int128>(width) * e, static_cast<__int128>(ld) * e};
+}
+
+// Whether two tensors share a byte; null ones do not. Rows of one stride may lie between those of
+// the other tensor (the halves of a product). Rows of two strides are not followed: they are
+// taken as apart unless they start together.
+bool share(Span a, Span b) {
+  if (a.at == nullptr || b.at == nullptr) return false;
+  const __int128 d = static_cast<__int128>(reinterpret_cast<uintptr_t>(b.at)) -
+                     static_cast<__int128>(reinterpret_cast<uintptr_t>(a.at));  // b begins d after a
+  const auto length = [](const Span& s) { return (s.rows - 1) * s.pitch + s.row; };
+  if (d >= length(a) || -d >= length(b)) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  // one row: of the other's pitch if it fits between two of its rows, else it meets one
+  Span* const one = a.rows == 1 ? &a : b.rows == 1 ? &b : nullptr;
+  if (one != nullptr) {
+    const Span& many = one == &a ? b : a;
+    if (one->row > many.pitch - many.row) return true;
+    one->pitch = many.pitch;
+  }
+  if (a.pitch != b.pitch) return d == 0;
+  __int128 q = d / a.pitch, r = d % a.pitch;  // row j of b begins r bytes after row j + q of a does
+  if (r < 0) {
+    r += a.pitch;
+    q -= 1;
+  }
+  const auto meet = [&](__int128 k) { return k > -b.rows && k < a.rows; };  // a row j of b and row j + k of a
+  return (r < a.row && meet(q)) || (r + b.row > a.pitch && meet(q + 1));
+}
+
+// Whether no output shares memory with an input or another output.
+bool apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+  for (const Span* o = outputs.begin(); o != outputs.end(); ++o) {
+    for (const Span& i : inputs)
+      if (share(*o, i)) return false;
+    for (const Span* p = outputs.begin(); p != o; ++p)
+      if (share(*o, *p)) return false;
+  }
+  return true;
+}
 
 dlvm_status overlap() { return fail(DLVM_ERR_INVALID_ARG, "an output must not overlap an input or another output"); }
 
@@ -84,7 +135,9 @@ dlvm_status dlvm_embedding_forward(int32_t dtype, int64_t vocab, int64_t width, 
   if (table == nullptr || ids == nullptr || out == nullptr)
     return fail(DLVM_ERR_INVALID_ARG, "null argument");
   if (!all_aligned16(table, ids, out)) return misaligned();
-  if (is_one_of(out, table, ids)) return overlap();
+  if (!apart({strided(out, dtype, tokens, width, width)},
+             {strided(table, dtype, vocab, width, width), piece(ids, tokens, 4)}))
+    return overlap();
   const hipError_t e = dlvm::launch_embedding_forward(dtype, vocab, width, tokens, table, ids, scale,
                                                       out, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? DLVM_OK : hip_fail(e, "embedding launch");
@@ -109,7 +162,10 @@ dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width,
   if (ws == nullptr || ws_bytes < dlvm::embedding_backward_ws(vocab, width, tokens))
     return fail(DLVM_ERR_WORKSPACE, "workspace missing or too small");
   if (!all_aligned16(ids, dout, dtable, ws)) return misaligned();
-  if (is_one_of(dtable, ids, dout)) return overlap();
+  if (!apart({piece(dtable, vocab * width, 4),
+              piece(ws, static_cast<int64_t>(dlvm::embedding_backward_ws(vocab, width, tokens)), 1)},
+             {piece(ids, tokens, 4), strided(dout, dtype, tokens, width, width)}))
+    return overlap();
   const hipError_t e = dlvm::launch_embedding_backward(dtype, vocab, width, tokens, ids, dout, scale,
                                                        accumulate != 0, dtable, ws,
                                                        static_cast<hipStream_t>(stream));
@@ -135,7 +191,12 @@ dlvm_status dlvm_gated_scan_forward(int32_t dtype, int32_t mode, int64_t steps, 
   if (ws != nullptr && ws_bytes < dlvm::gated_scan_ws(dtype, steps, batch, width))
     return fail(DLVM_ERR_WORKSPACE, "workspace is smaller than dlvm_gated_scan_ws_bytes");
   if (!all_aligned16(z, x, h0, lens, hs, hT, ws)) return misaligned();
-  if (is_one_of(hs, z, x)) return overlap();
+  const int64_t rows = steps * batch, states = batch * width;
+  if (!apart({strided(hs, dtype, rows, width, ldh), piece(hT, states, 4),
+              piece(ws, static_cast<int64_t>(dlvm::gated_scan_ws(dtype, steps, batch, width)), 1)},
+             {strided(z, dtype, rows, width, ldz), strided(x, dtype, rows, width, ldx),
+              piece(h0 == hT ? nullptr : h0, states, 4), piece(lens, batch, 4)}))
+    return overlap();
   dlvm::GatedScan c{};
   c.dtype = dtype;
   c.coupled = mode == DLVM_SCAN_COUPLED;
@@ -165,7 +226,13 @@ dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps,
   if (ws != nullptr && ws_bytes < dlvm::gated_scan_ws(dtype, steps, batch, width))
     return fail(DLVM_ERR_WORKSPACE, "workspace is smaller than dlvm_gated_scan_ws_bytes");
   if (!all_aligned16(z, x, h0, lens, hs, dhs, dhT, dz, dx, dh0, ws)) return misaligned();
-  if (is_one_of(dz, z, x, hs, dhs) || is_one_of(dx, z, x, hs, dhs, dz)) return overlap();
+  const int64_t rows = steps * batch, states = batch * width;
+  if (!apart({strided(dz, dtype, rows, width, lddz), strided(dx, dtype, rows, width, lddx), piece(dh0, states, 4),
+              piece(ws, static_cast<int64_t>(dlvm::gated_scan_ws(dtype, steps, batch, width)), 1)},
+             {strided(z, dtype, rows, width, ldz), strided(x, dtype, rows, width, ldx),
+              strided(hs, dtype, rows, width, ldh), strided(dhs, dtype, rows, width, lddh),
+              piece(h0, states, 4), piece(lens, batch, 4), piece(dhT == dh0 ? nullptr : dhT, states, 4)}))
+    return overlap();
   dlvm::GatedScan c{};
   c.dtype = dtype;
   c.coupled = mode == DLVM_SCAN_COUPLED;
@@ -202,6 +269,11 @@ dlvm_status dlvm_token_logprobs(int32_t dtype, int64_t rows, int64_t classes, co
   if (ws != nullptr && ws_bytes < dlvm::token_scores_ws(rows, classes, top))
     return fail(DLVM_ERR_WORKSPACE, "workspace is smaller than dlvm_token_logprobs_ws_bytes");
   if (!all_aligned16(logits, tokens, logp, lse, entropy, top_ids, top_logp, ws)) return misaligned();
+  if (!apart({piece(logp, rows, 4), piece(lse, rows, 4), piece(entropy, rows, 4), piece(top_ids, rows * top, 4),
+              piece(top_logp, rows * top, 4),
+              piece(ws, static_cast<int64_t>(dlvm::token_scores_ws(rows, classes, top)), 1)},
+             {strided(logits, dtype, rows, classes, ld), piece(tokens, rows, 4)}))
+    return overlap();
   const dlvm::TokenScores c{dtype, rows, classes, logits, ld, scale, tokens, logp, lse, entropy,
                             top, top_ids, top_logp};
   const hipError_t e = dlvm::launch_token_scores(c, ws, static_cast<hipStream_t>(stream));
@@ -228,6 +300,10 @@ dlvm_status dlvm_token_logprobs_backward(int32_t dtype, int32_t out_dtype, int64
   if (dlogits == logits && (dtype != out_dtype || ld != ld_out))
     return fail(DLVM_ERR_INVALID_ARG, "a gradient in place has the type and stride of the logits");
   if (!all_aligned16(logits, tokens, lse, entropy, dlogp, dentropy, dlogits)) return misaligned();
+  if (!apart({strided(dlogits, out_dtype, rows, classes, ld_out)},
+             {strided(dlogits == logits ? nullptr : logits, dtype, rows, classes, ld), piece(tokens, rows, 4),
+              piece(lse, rows, 4), piece(entropy, rows, 4), piece(dlogp, rows, 4), piece(dentropy, rows, 4)}))
+    return overlap();
   const hipError_t e = dlvm::launch_token_scores_backward(dtype, out_dtype, rows, classes, logits, ld,
                                                           scale, tokens, lse, entropy, dlogp,
                                                           dentropy, dlogits, ld_out,
