@@ -511,6 +511,10 @@ dlvm_status dlvm_embedding_backward(int32_t dtype, int64_t vocab, int64_t width,
  * a padded batch, taken as clamped to [0, steps]: steps t >= lens[b] leave the
  * state as it is, their z and x are not used (whatever they hold) and their hs
  * rows are zero. Columns width .. ld of a row are not touched.
+ * An infinity or a NaN in h0 or in x of a live step, or a NaN in its z, makes
+ * every state that it reaches infinite or NaN (which of the two depends on the
+ * sizes: steps are composed in another order) and no other; adjoints likewise,
+ * backwards. (A z of +-infinity is a gate of 1 or 0.)
  * `ws` (dlvm_gated_scan_ws_bytes, or NULL) lets a call with few columns and
  * many steps be cut into segments of time that run side by side and are then
  * joined; with NULL no call is cut. batch * width and batch * steps at most
