@@ -546,7 +546,7 @@ dlvm_status dlvm_gated_scan_backward(int32_t dtype, int32_t mode, int64_t steps,
                                      void* stream);
 
 /* Scores of tokens under logits [rows, classes] (`dtype`, row stride ld >=
- * classes): with y = scale * logits (scale > 0 and finite, an inverse
+ * classes): with y = scale * logits (scale > 0, at most 2e38, an inverse
  * temperature) and p = softmax(y), all outputs float32 unless said:
  *   logp[i]     y[i, tokens[i]] - lse[i]; 0 where tokens[i] is -1, NaN for any
  *               other token outside [0, classes). tokens and logp NULL: none.

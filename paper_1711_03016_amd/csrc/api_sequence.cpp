@@ -20,6 +20,8 @@ constexpr int64_t kMaxWidth = int64_t(1) << 20;
 constexpr int64_t kMaxRows = INT32_MAX;
 // Strides beyond this could take a row's offset past 63 bits.
 constexpr int64_t kMaxStride = int64_t(1) << 31;
+// The scale of scores is multiplied by log2(e) in float32.
+constexpr float kMaxScale = 2e38f;
 
 dlvm_status embedding_sizes(int32_t dtype, int64_t vocab, int64_t width, int64_t tokens, float scale) {
   if (!valid_dtype(dtype)) return fail(DLVM_ERR_INVALID_ARG, "bad dtype");
@@ -59,6 +61,7 @@ dlvm_status score_sizes(int32_t dtype, int64_t rows, int64_t classes, int64_t ld
   if (!std::isfinite(scale) || scale <= 0) return fail(DLVM_ERR_INVALID_ARG, "scale must be finite and positive");
   if (rows > kMaxRows || classes > (int64_t(1) << 30) || ld > kMaxStride)
     return fail(DLVM_ERR_UNSUPPORTED, "rows below 2^31, classes at most 2^30, row strides at most 2^31");
+  if (scale > kMaxScale) return fail(DLVM_ERR_UNSUPPORTED, "scale at most 2e38");
   return DLVM_OK;
 }
 
