@@ -667,28 +667,31 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
 // Choice of the variant, for N states: alone where a thread to each state fills the GPU for
 // so few steps, chained, or in segments, where the tiles of states leave compute units idle
 // for so many steps that it pays for another launch and the waiting, or the second reading.
-// Forward and gradient in us, bf16, T steps of so many tiles of 64 states:
-//                          alone         shared
-//   1024 tiles, T 16    4.4 and 5.9    6.9 and 12.1
-//   512 tiles, T 32     5.8 and 8.3    5.0 and 7.7
-//   1024 tiles, T 32    6.4 and 9.6    7.4 and 12.5
-//   1024 tiles, T 64    9.1 and 15.9   8.4 and 12.8
-//   2048 tiles, T 64   15.1 and 23.9  13.4 and 23.6
-//   2048 tiles, T 128  26.8 and 45.4  23.1 and 40.1
-//   4096 tiles, T 64   23.0 and 35.8  24.7 and 45.4
+// Forward and gradient in us, bf16, T steps of so many tiles of 64 states (a training step takes
+// both, so their sum decides):
+//                          alone          shared
+//   1024 tiles, T 16    4.4 and 6.5    6.1 and 16.2
+//   512 tiles, T 32     5.7 and 10.1   4.4 and 9.6
+//   1024 tiles, T 32    6.1 and 11.4   7.0 and 16.0
+//   1024 tiles, T 64    9.4 and 18.4   7.7 and 16.5
+//   2048 tiles, T 64   14.3 and 29.2  13.5 and 30.2   (float32 22.2 and 28.7, 23.8 and 36.5)
+//   2048 tiles, T 128  26.4 and 54.5  23.7 and 54.1
+//   4096 tiles, T 64   23.4 and 44.0  24.9 and 58.2
 // Forward, bf16, in one piece against chained: 8 tiles, T 1024 20.8 and 9.5, T 16384 295 and
 // 21; 128 tiles, T 1024 22 and 16, T 4096 76 and 44; 188 tiles, T 1024 24 and 27, T 2048 43
-// and 43. Gradient in one piece against segments: 128 tiles, T 2048 80 and 54; 160 tiles,
-// T 777 36 and 31, T 300 16 and 18; 204 tiles, T 777 39 and 39, in float32 47 and 50. Where
-// sequences end at lengths the longest hold a few compute units longest: 204 tiles, T 777,
-// float32 50 and 46; 192 tiles, T 2048 87 and 70; 320 tiles, T 2048 132 and 114; 384 tiles,
-// T 1024, float32 92 and 102.
+// and 43. Gradient in one piece against segments, both launches: bf16, 128 tiles, T 2048 106 and
+// 73; 160 tiles, T 777 46 and 37; 204 tiles, T 777 50 and 59, in float32 44 and 52. Few
+// steps do not pay: 160 tiles, T 300 20 and 25, in float32 16 and 19, 8 tiles 18.0 and 18.8.
+// Where sequences end at lengths the longest hold a few compute
+// units longest: 192 tiles, T 2048 105 and 95; 320 tiles, T 2048 158 and 159, in float32 179
+// and 166; 384 tiles, T 1024, float32 89 and 100.
 // ---------------------------------------------------------------------------
 constexpr int64_t kBlocks = 512;       // two workgroups on a compute unit
 constexpr int64_t kUncut = 192;        // tiles from which a gradient is not cut
 constexpr int64_t kUncutRagged = 352;  // where sequences have lengths
 constexpr int64_t kUnchained = 160;    // and a forward call not chained
 constexpr int32_t kShortest = 128;     // steps of a segment at least
+constexpr int64_t kCutSteps = 384;     // steps from which a gradient is cut
 
 bool alone(int64_t T, int64_t N) {
   const int64_t tiles = (N + 63) / 64;
@@ -703,7 +706,7 @@ int segments(int64_t T, int64_t N, bool ragged, int32_t* len) {
   const int64_t tiles = (N + 63) / 64, step = kWaves * kUnroll;
   int64_t S = alone(T, N) || tiles >= (ragged ? kUncutRagged : kUncut) ? 1 : (kBlocks + tiles - 1) / tiles;
   if (S > T / kShortest) S = T / kShortest;
-  if (S < 1) S = 1;
+  if (T < kCutSteps) S = 1;
   const int64_t L = S == 1 ? T : ((T + S - 1) / S + step - 1) / step * step;
   *len = static_cast<int32_t>(L);
   return static_cast<int>((T + L - 1) / L);

@@ -112,7 +112,8 @@ def _compare(got, z, x, h0, lens, dhs, dhT, dtype, mode, keep):
 # About the eight steps of a thread and the 64 of a workgroup, a thread through many steps, one
 # workgroup through many rounds, segments.
 SIZES = [(8, 2, 64), (9, 5, 63), (16, 2, 130), (17, 3, 64), (32, 64, 1024), (33, 40, 96), (64, 300, 64),
-         (65, 2, 24), (129, 1, 40), (300, 2, 257), (1000, 1, 96), (1025, 3, 33), (2100, 3, 40)]
+         (65, 2, 24), (129, 1, 40), (300, 2, 257), (383, 2, 72), (384, 2, 72), (1000, 1, 96), (1025, 3, 33),
+         (2100, 3, 40)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -129,7 +130,8 @@ def test_gradient_where_the_state_follows_the_input(dtype, mode, size):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("size", [(13, 6, 64), (40, 4100, 64), (130, 5, 40), (300, 200, 64), (700, 9, 72)])
+@pytest.mark.parametrize("size", [(13, 6, 64), (40, 4100, 64), (130, 5, 40), (300, 200, 64), (700, 9, 72),
+                                  (400, 200, 64), (520, 257, 64)])
 def test_padded_gradient_where_the_state_follows_the_input(dtype, size):
     """Lengths of zero, one, about a round and all; what dead steps hold is not used. A thread
     through many rounds, and a gradient that is cut only because sequences have lengths."""
