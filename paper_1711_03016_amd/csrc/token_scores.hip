@@ -630,7 +630,7 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
 //                   1      4      8
 //   256 x 1500     6.5           6.2
 //   1024 x 1500    6.6          10.8
-//   512 x 4000     9.8    6.4    7.2
+//   512 x 4000     9.8    6.4    7.2   (700 x 4000 6.8 and 8.3, 512 x 8000 8.4 and 8.2)
 //   512 x 131072  89     36     32
 //   1024 x 4000   10.3    7.5   11.1
 //   1024 x 131072 94     54     55
@@ -650,7 +650,7 @@ __global__ __launch_bounds__(256) void dlvm_token_scores_grad_kernel(ScoresGrad 
 constexpr int64_t kWaveRow = 2048;      // classes up to which a wave takes a row
 constexpr int64_t kWaveRows = 4096;     // rows from which it takes one
 constexpr int64_t kWaveRowOfMany = 16384;  // of up to so many classes
-constexpr int64_t kFourRows = 768;      // rows from which four waves take one, else eight,
+constexpr int64_t kFourRows = 512;      // rows from which four waves take one, else eight,
 constexpr int64_t kFourBytes = 96 << 10;  // if it has up to so many bytes
 constexpr int64_t kCutRow = 32768;      // classes from which a row is cut into parts,
 constexpr int64_t kCutPlain = 98304;    // or these without alternatives,
