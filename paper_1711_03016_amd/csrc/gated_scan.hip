@@ -36,9 +36,9 @@ constexpr int kWaves = 8;          // waves of a workgroup that share the steps
 constexpr int kUnroll = 8;         // steps of a thread that are in flight together
 constexpr int kChainedUnroll = 32; // and in a block of a chain
 
-// a = sigmoid(z) and c = 1 - a, each to float32 accuracy on its own (1 - a from a
-// rounded a loses its digits where the gate is open). z of +-infinity gives 0 and 1, NaN
-// stays NaN.
+// a = sigmoid(z) and c = 1 - a, each with its own relative error (1 - a from a rounded a
+// loses its digits where the gate is open): below (|z| + 16) 2^-23, since the argument of the
+// exponential is rounded. z of +-infinity gives 0 and 1, NaN stays NaN.
 __device__ __forceinline__ void gate(float z, float& a, float& c) {
   const float e = __builtin_amdgcn_exp2f(z * -1.44269504088896340736f);
   a = __builtin_amdgcn_rcpf(1.0f + e);
@@ -67,7 +67,8 @@ struct Cut {
 // and the lane's state, first kEmpty, then the block's map (A, Q), then (kState, the state
 // after it): 64 bits that are written and read whole, so that a word needs no flag beside it
 // and no order with other memory. (A is a product of gates, never negative; a NaN is stored
-// as the one that is not kEmpty.)
+// as the one that is not kEmpty.) This is the decoupled look-back of the single-pass prefix
+// sums of D. Merrill and M. Garland (2016), for maps in place of sums.
 //
 // A workgroup takes the next block of its tile by a ticket, so every earlier block is
 // taken by a workgroup that runs already, and that publishes its map without waiting for
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
 // off by: there a pass forwards through z and x finds those states in float32 first, and keeps
 // each in the two bf16 of dz and dx at its first step until the same thread comes back to it
 // and writes the gradients. (The gradient of 32 steps of 2^20 states takes 84 us with that pass
-// and 70 with the rows of hs, 4096 steps of 8192 states 144 and 102.)
+// and 70 with the rows of hs, 4096 steps of 8192 states 139 and 102.)
 // ---------------------------------------------------------------------------
 template <typename E> constexpr bool kRecompute = sizeof(E) == 2;
 
