@@ -483,7 +483,7 @@ __global__ __launch_bounds__(MODE == ALONE ? 256 : 64 * kWaves) void dlvm_gated_
     if (t0 < begin) return;
     const int32_t from = t0 < stop ? t0 : stop;
     auto rz = pz.row(from), rx = px.row(from), rd = pd.row(from);
-    if constexpr (kRecompute<E>)
+    if constexpr (kRecompute<E>)  // of steps behind the last live one: any row, not used
       before = __uint_as_float(static_cast<uint32_t>(gz.in(gz.row(from))) << 16 |
                                static_cast<uint32_t>(gx.in(gx.row(from))));
     else
@@ -683,9 +683,9 @@ __global__ __launch_bounds__(64 * kWaves) void dlvm_gated_scan_sums_kernel(Gated
 // and 43. Gradient in one piece against segments, both launches: bf16, 128 tiles, T 2048 106 and
 // 73; 160 tiles, T 777 46 and 37; 204 tiles, T 777 50 and 59, in float32 44 and 52. Few
 // steps do not pay: 160 tiles, T 300 20 and 25, in float32 16 and 19, 8 tiles 18.0 and 18.8.
-// Where sequences end at lengths the longest hold a few compute
-// units longest: 192 tiles, T 2048 105 and 95; 320 tiles, T 2048 158 and 159, in float32 179
-// and 166; 384 tiles, T 1024, float32 89 and 100.
+// Where sequences end at lengths the longest hold a few compute units longest: 192 tiles,
+// T 2048 105 and 95; 320 tiles, T 2048 158 and 159, in float32 179 and 166; 384 tiles, T 1024,
+// float32 89 and 100.
 // ---------------------------------------------------------------------------
 constexpr int64_t kBlocks = 512;       // two workgroups on a compute unit
 constexpr int64_t kUncut = 192;        // tiles from which a gradient is not cut
